@@ -82,6 +82,8 @@ typedef enum sp_prune_mode { SP_ACCEPT = 0, SP_DROP = 1, SP_CLEAR = 2 } sp_prune
 #define SP_FLAG_PACKED_WEIGHTS 2u   /* wqkv, wo, wgu, wd were re-laid by sp_pack_weights() (bf16 MFMA path only) */
 #define SP_FLAG_NO_GRAPHS 8u        /* never replay HIP graphs inside sp_stage_forward (see there) */
 #define SP_FLAG_PAGED_KV 4u         /* requests hold their cache in pages of page_slots slots (see below) */
+#define SP_FLAG_FP4_WEIGHTS 16u     /* wqkv, wo, wgu, wd were packed by sp_fp4_pack_weights() (see "4-bit storage") */
+#define SP_FLAG_FP4_KV 32u          /* the cache holds K and V in 4 bits (see "4-bit storage") */
 
 typedef struct sp_config {
   int32_t n_layers;
@@ -110,6 +112,12 @@ typedef struct sp_layer_weights {
   const void* norm1;   /* [d_model] gain of the attention RMSNorm */
   const void* norm2;   /* [d_model] gain of the FFN RMSNorm       */
 } sp_layer_weights;
+
+/* Device pointers of one layer's head norms (storage type of the config, 16-byte aligned). */
+typedef struct sp_head_norms {
+  const void* q;       /* [d_head] gain of the query heads' RMSNorm */
+  const void* k;       /* [d_head] gain of the key heads' RMSNorm   */
+} sp_head_norms;
 
 typedef struct sp_sizes {
   size_t kv_bytes;         /* KV slab */
@@ -209,6 +217,60 @@ int sp_request_release(sp_stage* stage, int32_t req, sp_stream stream);
 /* Pages not held by any request (SP_E_INVALID for a null stage). */
 int sp_stage_free_pages(const sp_stage* stage);
 
+/* ---- 4-bit storage ------------------------------------------------------------
+ *
+ * Weights, the K/V cache, or both may be held in 4 bits (bf16 stages only).  32 consecutive values (of a weight row,
+ * of a cache row's head) share a power of two 2^e, the smallest with max |x| <= 6 * 2^e and -100 <= e <= 125; a value
+ * is one of +-{0, 0.5, 1, 1.5, 2, 3, 4, 6} * 2^e, rounded to nearest, ties to the even code.  4.25 bits a value in
+ * weights, 4.25 (d_head 128) or 4.5 (64) in the cache.  Every held value is exact in bf16: products and attention
+ * over 4-bit storage are those over the held values, with sums, softmax statistics and norms in float32.  An infinity
+ * is held as +-6 * 2^125, a NaN as zero; what is read back is always finite.
+ *
+ * SP_FLAG_FP4_KV: d_head 64 or 128, any stage shape.  The slab holds d_head / 2 bytes of codes per (slot, head) row in
+ * the layout above and, behind all code planes, four bytes of scales per row in planes of the same order; it is written
+ * and read through sp_kv_store, sp_kv_load, sp_stage_append and sp_stage_forward (sp_sizes reports the code planes).
+ * Inserting, pruning, compaction and pages work as for the other caches.
+ * SP_FLAG_FP4_WEIGHTS: the shapes SP_FLAG_PACKED_WEIGHTS takes, not together with it; the vocabulary matrix of the
+ * output head stays bf16, row-major. */
+
+/* Bytes of a packed [n_rows][n_cols] matrix; 0 if it cannot be packed: n_rows % 16 == 0, n_cols % 32 == 0, both up to
+ * SP_FP4_MAX_DIM.  (Storage is in pieces of 16 rows x 256 columns: a last piece may be part empty.) */
+#define SP_FP4_MAX_DIM (1 << 17)
+size_t sp_fp4_matrix_bytes(int32_t n_rows, int32_t n_cols);
+
+/* Load-time conversion of a bf16 [n_rows][n_cols] matrix to 4 bits, and back to the bf16 values held.  Pointers are
+ * 16-byte aligned, `out` is caller-allocated and distinct from `in`.  Errors: SP_E_INVALID, SP_E_UNSUPPORTED (shape). */
+int sp_fp4_pack_matrix(const void* in /*device*/, void* out /*device*/, int32_t n_rows, int32_t n_cols, sp_stream stream);
+int sp_fp4_unpack_matrix(const void* in /*device*/, void* out /*device*/, int32_t n_rows, int32_t n_cols, sp_stream stream);
+
+/* The four projection matrices of one layer; `out` buffers of sp_fp4_matrix_bytes() each ([rows][columns] as in
+ * sp_layer_weights).  norm1 and norm2 are not touched.  Create the stage with SP_FLAG_FP4_WEIGHTS to use the result. */
+int sp_fp4_pack_weights(const sp_config* cfg, const sp_layer_weights* in, const sp_layer_weights* out, sp_stream stream);
+
+/* out = x W^T with a matrix of 4-bit weights: x bf16 [m][k], W packed [n][k], out bf16 [m][n]; any m, also a single row.
+ * gated = 1: W is packed [2 n][k], gate rows then up rows, and out = silu(x Wgate^T) * (x Wup^T), n % 16 == 0.
+ * All pointers are 16-byte aligned device memory; x and out may not overlap.  Small products cut the columns and join
+ * the pieces in `workspace` (contents need not persist; calls that overlap in time need one each), of at least
+ * sp_fp4_product_workspace() bytes, which may be 0.  m == 0 does nothing.  Errors: SP_E_INVALID, SP_E_UNSUPPORTED (shape),
+ * SP_E_CAPACITY (workspace). */
+size_t sp_fp4_product_workspace(int32_t m, int32_t n, int32_t k, int32_t gated);
+int sp_fp4_product(const void* x, int32_t m, const void* w, int32_t n, int32_t k, int32_t gated, void* out,
+                   void* workspace /*nullable if 0 bytes*/, size_t workspace_bytes, sp_stream stream);
+
+/* K and V rows of request `req`, [n][n_kv_heads][d_head] in the config dtype, 16-byte aligned device memory: stored into, or
+ * read from, the logical cache slots first_slot .. first_slot + n - 1 of one layer (the committed context first, then the
+ * tree's nodes), in whichever form the stage keeps its cache, pages included.  K rows are stored as they are given (rotated).
+ * After sp_request_init this is the way to fill a committed context that 4 bits hold.  Errors: SP_E_BAD_REQ, SP_E_PENDING,
+ * SP_E_INVALID, SP_E_CAPACITY (slots past prefix_len + n_live). */
+int sp_kv_store(sp_stage* stage, int32_t req, int32_t layer, int32_t first_slot, int32_t n, const void* k, const void* v,
+                sp_stream stream);
+int sp_kv_load(sp_stage* stage, int32_t req, int32_t layer, int32_t first_slot, int32_t n, void* k, void* v, sp_stream stream);
+
+/* Head norms: from here on the stage's query and key heads pass RMSNorm(x; gain, rms_eps) over their d_head columns, in
+ * float32, before the rotation, in sp_stage_forward and sp_stage_append.  `layers` is a host array of n_layers entries holding
+ * device pointers, which must stay valid; NULL: none (the state after sp_stage_create).  Errors: SP_E_INVALID. */
+int sp_stage_set_head_norms(sp_stage* stage, const sp_head_norms* layers);
+
 /* ---- the hot path ------------------------------------------------------------ */
 
 /* Layer appending (Sec. 3.2): appends n_new nodes to request `req`.  parents[k] is
@@ -247,6 +309,23 @@ int sp_tree_insert_batch(sp_stage* stage, int32_t n_req, const int32_t* req_ids 
 int sp_stage_forward(sp_stage* stage, int32_t n_req, const int32_t* req_ids /*host*/,
                      const int32_t* first_node /*host*/, const int32_t* n_nodes /*host*/,
                      const void* x_in /*device*/, void* x_out /*device*/, sp_stream stream);
+
+/* The attention of one layer piece by piece, for layers whose other parts the caller computes (its own projections or mixing):
+ * the same rows, order and errors as sp_stage_forward, plus SP_E_INVALID for a layer outside the stage.
+ * sp_stage_append takes the rows of the QKV projection, [sum n_nodes][(n_q + 2 n_kv) * d_head] in the config dtype (query
+ * heads, key heads, value heads): norms of the query and key heads where the stage has them, rotation at prefix_len + depth,
+ * K and V into the nodes' cache slots, the queries to q_out [sum n_nodes][n_q * d_head], in one launch.  Appending to the
+ * stage's last layer makes the nodes count as forwarded.
+ * sp_stage_attention computes the tree attention of such queries over what the layer's cache holds: softmax(q K^T /
+ * sqrt(d_head)) V over the committed context, the node itself and its ancestors; out [sum n_nodes][n_q * d_head], which may
+ * not overlap q.  Rows of the cache that nothing was appended to since their node was inserted hold zeros.
+ * qkv, q, q_out and out are 16-byte aligned device memory.  sp_stage_attention uses the stage's workspace. */
+int sp_stage_append(sp_stage* stage, int32_t layer, int32_t n_req, const int32_t* req_ids /*host*/,
+                    const int32_t* first_node /*host*/, const int32_t* n_nodes /*host*/, const void* qkv, void* q_out,
+                    sp_stream stream);
+int sp_stage_attention(sp_stage* stage, int32_t layer, int32_t n_req, const int32_t* req_ids /*host*/,
+                       const int32_t* first_node /*host*/, const int32_t* n_nodes /*host*/, const void* q, void* out,
+                       sp_stream stream);
 
 /* Pruning propagation, table part (Sec. 3.2, Algorithm 1 lines 5 and 7).
  * SP_ACCEPT(node): the verified token is `node`.  The path root..node joins the

@@ -25,6 +25,8 @@ SP_FLAG_SIMPLE_KERNELS = 1
 SP_FLAG_PACKED_WEIGHTS = 2
 SP_FLAG_PAGED_KV = 4
 SP_FLAG_NO_GRAPHS = 8
+SP_FLAG_FP4_WEIGHTS = 16
+SP_FLAG_FP4_KV = 32
 
 # sp_kernel_kind
 K_GEMM_QKV, K_GEMM_O, K_GEMM_GATEUP, K_GEMM_DOWN = 1, 2, 3, 4
@@ -51,6 +53,10 @@ class sp_config(C.Structure):
 
 class sp_layer_weights(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("wqkv", "wo", "wgu", "wd", "norm1", "norm2")]
+
+
+class sp_head_norms(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p)]
 
 
 class sp_sizes(C.Structure):
@@ -97,6 +103,15 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
                             C.POINTER(vp)],
         "sp_pack_weights": [C.POINTER(sp_config), C.POINTER(sp_layer_weights), C.POINTER(sp_layer_weights), vp],
         "sp_pack_matrix": [vp, vp, C.c_int32, C.c_int32, vp],
+        "sp_fp4_pack_matrix": [vp, vp, C.c_int32, C.c_int32, vp],
+        "sp_fp4_unpack_matrix": [vp, vp, C.c_int32, C.c_int32, vp],
+        "sp_fp4_pack_weights": [C.POINTER(sp_config), C.POINTER(sp_layer_weights), C.POINTER(sp_layer_weights), vp],
+        "sp_fp4_product": [vp, C.c_int32, vp, C.c_int32, C.c_int32, C.c_int32, vp, vp, C.c_size_t, vp],
+        "sp_kv_store": [vp, C.c_int32, C.c_int32, C.c_int32, C.c_int32, vp, vp, vp],
+        "sp_kv_load": [vp, C.c_int32, C.c_int32, C.c_int32, C.c_int32, vp, vp, vp],
+        "sp_stage_set_head_norms": [vp, C.POINTER(sp_head_norms)],
+        "sp_stage_append": [vp, C.c_int32, C.c_int32, i32p, i32p, i32p, vp, vp, vp],
+        "sp_stage_attention": [vp, C.c_int32, C.c_int32, i32p, i32p, i32p, vp, vp, vp],
         "sp_request_init": [vp, C.c_int32, C.c_int64, C.c_int32, C.c_int32, vp],
         "sp_stage_verify_head": [vp, C.POINTER(sp_head_weights), C.c_int32, i32p, i32p, i32p, vp, vp, vp, vp],
         "sp_stage_verify_head_noalloc": [vp, C.POINTER(sp_head_weights), C.c_int32, i32p, i32p, i32p, vp, vp, vp, vp],
@@ -130,6 +145,10 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
         fn = getattr(lib, name)
         fn.argtypes = args
         fn.restype = C.c_int
+    lib.sp_fp4_matrix_bytes.argtypes = [C.c_int32, C.c_int32]
+    lib.sp_fp4_matrix_bytes.restype = C.c_size_t
+    lib.sp_fp4_product_workspace.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.c_int32]
+    lib.sp_fp4_product_workspace.restype = C.c_size_t
     lib.sp_stage_destroy.argtypes = [vp]
     lib.sp_stage_destroy.restype = None
     lib.sp_strerror.argtypes = [C.c_int]
@@ -173,7 +192,7 @@ class Stage:
 
     def __init__(self, shape, layers: List[Dict[str, "object"]], *, kv_slots: int, max_requests: int = 1,
                  max_batch_nodes: int = 64, max_tree_nodes: int = SP_MAX_TREE_NODES, flags: int = 0,
-                 device: str = "cuda:0", page_slots: int = 0):
+                 device: str = "cuda:0", page_slots: int = 0, head_norms: Optional[List[Dict[str, "object"]]] = None):
         import torch
         self.torch = torch
         self.lib = load_library()
@@ -197,7 +216,13 @@ class Stage:
         for l, w in enumerate(layers):
             for name in ("wqkv", "wo", "wgu", "wd", "norm1", "norm2"):
                 t = w[name]
-                assert t.is_cuda and t.is_contiguous() and t.dtype == self.tdtype, name
+                if flags & SP_FLAG_FP4_WEIGHTS and not name.startswith("norm"):
+                    rows, cols = self._matrix_shape(name)
+                    assert isinstance(t, Fp4Matrix) and (t.n_rows, t.n_cols) == (rows, cols), name
+                    t = t.data
+                    assert t.is_cuda and t.is_contiguous(), name
+                else:
+                    assert t.is_cuda and t.is_contiguous() and t.dtype == self.tdtype, name
                 setattr(arr[l], name, t.data_ptr())
         bufs = sp_buffers(self.kv.data_ptr(), sz.kv_bytes, self.tables.data_ptr(), sz.tables_bytes,
                           self.workspace.data_ptr(), sz.workspace_bytes)
@@ -205,6 +230,8 @@ class Stage:
         _check(self.lib.sp_stage_create(C.byref(self.cfg), arr, C.byref(bufs), self._stream(), C.byref(h)),
                "sp_stage_create")
         self.handle = h
+        if head_norms is not None:
+            self.set_head_norms(head_norms)
 
     # -- plumbing -----------------------------------------------------------------
     def _stream(self):
@@ -225,9 +252,16 @@ class Stage:
         except Exception:
             pass
 
+    def _matrix_shape(self, name: str):
+        s = self.shape
+        return {"wqkv": ((s.n_q_heads + 2 * s.n_kv_heads) * s.d_head, s.d_model), "wo": (s.d_model, s.n_q_heads * s.d_head),
+                "wgu": (2 * s.d_ff, s.d_model), "wd": (s.d_model, s.d_ff)}[name]
+
     def kv_view(self):
         """The slab as a tensor [layer, K|V, kv_head, slot, d_head] (no copy)."""
         s = self.shape
+        if self.cfg.flags & SP_FLAG_FP4_KV:
+            raise ValueError("a cache in 4 bits is read and written through kv_load and kv_store")
         return self.kv.view(self.tdtype).view(s.n_layers, 2, s.n_kv_heads, self.cfg.kv_slots, s.d_head)
 
     # -- the C ABI, one method per entry point --------------------------------------
@@ -293,6 +327,66 @@ class Stage:
         _check(self.lib.sp_stage_forward(self.handle, len(ra), rp, fp, np_, C.c_void_p(x_in.data_ptr()),
                                          C.c_void_p(x_out.data_ptr()), self._stream()), "sp_stage_forward")
         return x_out
+
+    # -- the attention of a layer piece by piece, and cache rows ------------------------------
+    def set_head_norms(self, norms: Optional[List[Dict[str, "object"]]]):
+        """norms: per layer {"q": tensor [d_head], "k": tensor [d_head]}, or None for a model without head norms."""
+        arr = None
+        if norms is not None:
+            assert len(norms) == self.shape.n_layers
+            arr = (sp_head_norms * self.shape.n_layers)()
+            for l, w in enumerate(norms):
+                for name in ("q", "k"):
+                    t = w[name]
+                    assert t.is_cuda and t.is_contiguous() and t.dtype == self.tdtype and t.shape == (self.shape.d_head,), name
+                    setattr(arr[l], name, t.data_ptr())
+        _check(self.lib.sp_stage_set_head_norms(self.handle, arr), "sp_stage_set_head_norms")
+        self.head_norms = norms                  # keeps the gains alive
+
+    def _rows_tensor(self, t, rows: int, cols: int):
+        assert t.is_cuda and t.is_contiguous() and t.dtype == self.tdtype and t.shape == (rows, cols)
+        return C.c_void_p(t.data_ptr())
+
+    def append(self, layer: int, req_ids: Sequence[int], first_node: Sequence[int], n_nodes: Sequence[int], qkv, q_out=None):
+        """sp_stage_append: qkv [sum n_nodes, (n_q + 2 n_kv) * d_head] -> the rotated queries [sum n_nodes, n_q * d_head]."""
+        s = self.shape
+        ra, rp = _i32(req_ids)
+        fa, fp = _i32(first_node)
+        na, np_ = _i32(n_nodes)
+        rows, dq = int(sum(na)), s.n_q_heads * s.d_head
+        if q_out is None:
+            q_out = self.torch.empty(rows, dq, dtype=self.tdtype, device=self.device)
+        _check(self.lib.sp_stage_append(self.handle, layer, len(ra), rp, fp, np_,
+                                        self._rows_tensor(qkv, rows, dq + 2 * s.n_kv_heads * s.d_head),
+                                        self._rows_tensor(q_out, rows, dq), self._stream()), "sp_stage_append")
+        return q_out
+
+    def attention(self, layer: int, req_ids: Sequence[int], first_node: Sequence[int], n_nodes: Sequence[int], q, out=None):
+        """sp_stage_attention: q [sum n_nodes, n_q * d_head] -> the attention output of the same shape."""
+        ra, rp = _i32(req_ids)
+        fa, fp = _i32(first_node)
+        na, np_ = _i32(n_nodes)
+        rows, dq = int(sum(na)), self.shape.n_q_heads * self.shape.d_head
+        if out is None:
+            out = self.torch.empty(rows, dq, dtype=self.tdtype, device=self.device)
+        _check(self.lib.sp_stage_attention(self.handle, layer, len(ra), rp, fp, np_, self._rows_tensor(q, rows, dq),
+                                           self._rows_tensor(out, rows, dq), self._stream()), "sp_stage_attention")
+        return out
+
+    def kv_store(self, req: int, layer: int, first_slot: int, k, v):
+        """sp_kv_store: K and V rows [n, n_kv_heads, d_head] into logical slots first_slot .. first_slot + n - 1."""
+        s, n = self.shape, int(k.shape[0])
+        for t in (k, v):
+            assert t.is_cuda and t.is_contiguous() and t.dtype == self.tdtype and t.shape == (n, s.n_kv_heads, s.d_head)
+        _check(self.lib.sp_kv_store(self.handle, req, layer, first_slot, n, k.data_ptr(), v.data_ptr(), self._stream()), "sp_kv_store")
+
+    def kv_load(self, req: int, layer: int, first_slot: int, n: int):
+        """sp_kv_load: the K and V rows [n, n_kv_heads, d_head] that the cache holds."""
+        s = self.shape
+        k = self.torch.empty(max(n, 0), s.n_kv_heads, s.d_head, dtype=self.tdtype, device=self.device)
+        v = self.torch.empty_like(k)
+        _check(self.lib.sp_kv_load(self.handle, req, layer, first_slot, n, k.data_ptr(), v.data_ptr(), self._stream()), "sp_kv_load")
+        return k, v
 
     def tree_prune(self, req: int, mode: int, node: int):
         live, commit = C.c_int32(-1), C.c_int32(-1)
@@ -522,6 +616,92 @@ def pack_matrix(w, device: str = "cuda:0"):
     stream = C.c_void_p(torch.cuda.current_stream(torch.device(device)).cuda_stream)
     _check(lib.sp_pack_matrix(w.data_ptr(), out.data_ptr(), w.shape[0], w.shape[1], stream), "sp_pack_matrix")
     torch.cuda.synchronize()
+    return out
+
+
+# ---- 4-bit weights ------------------------------------------------------------------------
+class Fp4Matrix:
+    """A matrix of 4-bit weights: the packed bytes (a uint8 device tensor) and its shape."""
+
+    def __init__(self, data, n_rows: int, n_cols: int):
+        self.data, self.n_rows, self.n_cols = data, n_rows, n_cols
+
+
+def _raw_stream(device):
+    import torch
+    return C.c_void_p(torch.cuda.current_stream(device).cuda_stream)
+
+
+def _fp4_empty(n_rows: int, n_cols: int, device) -> Fp4Matrix:
+    import torch
+    size = load_library().sp_fp4_matrix_bytes(n_rows, n_cols)
+    if size == 0:
+        raise SpError(-9, "a %d x %d matrix in 4 bits" % (n_rows, n_cols))
+    return Fp4Matrix(torch.empty(size, dtype=torch.uint8, device=device), n_rows, n_cols)
+
+
+def fp4_pack_matrix(w) -> Fp4Matrix:
+    """sp_fp4_pack_matrix: a [rows, cols] bf16 device tensor in 4 bits."""
+    import torch
+    assert w.is_cuda and w.is_contiguous() and w.dtype == torch.bfloat16 and w.dim() == 2
+    out = _fp4_empty(int(w.shape[0]), int(w.shape[1]), w.device)
+    with torch.cuda.device(w.device):
+        _check(load_library().sp_fp4_pack_matrix(w.data_ptr(), out.data.data_ptr(), out.n_rows, out.n_cols, _raw_stream(w.device)),
+               "sp_fp4_pack_matrix")
+    return out
+
+
+def fp4_unpack_matrix(w: Fp4Matrix):
+    """sp_fp4_unpack_matrix: the bf16 values that the matrix holds."""
+    import torch
+    out = torch.empty(w.n_rows, w.n_cols, dtype=torch.bfloat16, device=w.data.device)
+    with torch.cuda.device(out.device):
+        _check(load_library().sp_fp4_unpack_matrix(w.data.data_ptr(), out.data_ptr(), w.n_rows, w.n_cols, _raw_stream(out.device)),
+               "sp_fp4_unpack_matrix")
+    return out
+
+
+def fp4_pack_weights(shape, layers: List[Dict[str, "object"]]):
+    """sp_fp4_pack_weights on every layer: new layer dicts whose four projection matrices are Fp4Matrix (create the
+    Stage with SP_FLAG_FP4_WEIGHTS).  The inputs can be dropped."""
+    import torch
+    lib = load_library()
+    cfg = sp_config(shape.n_layers, shape.d_model, shape.n_q_heads, shape.n_kv_heads, shape.d_head, shape.d_ff,
+                    shape.rms_eps, shape.rope_theta, SP_BF16, 1, SP_MAX_TREE_NODES, 1, 1, 0)
+    out = []
+    for w in layers:
+        o = dict(w)
+        a, b = sp_layer_weights(), sp_layer_weights()
+        for name in ("wqkv", "wo", "wgu", "wd"):
+            assert w[name].is_cuda and w[name].is_contiguous() and w[name].dtype == torch.bfloat16, name
+            o[name] = _fp4_empty(int(w[name].shape[0]), int(w[name].shape[1]), w[name].device)
+            setattr(a, name, w[name].data_ptr())
+            setattr(b, name, o[name].data.data_ptr())
+        device = w["wqkv"].device
+        with torch.cuda.device(device):
+            _check(lib.sp_fp4_pack_weights(C.byref(cfg), C.byref(a), C.byref(b), _raw_stream(device)), "sp_fp4_pack_weights")
+        out.append(o)
+    return out
+
+
+def fp4_product(x, w: Fp4Matrix, gated: bool = False, out=None):
+    """sp_fp4_product: x [m, k] bf16 times the held weights, [m, n]; gated: the first half of the matrix's rows are gates,
+    the second the up rows, and the result is silu(gate) * up, [m, n_rows / 2].  The workspace is torch's."""
+    import torch
+    lib = load_library()
+    if gated and w.n_rows % 32:
+        raise SpError(-9, "a gated product of %d rows" % w.n_rows)
+    n = w.n_rows // 2 if gated else w.n_rows
+    assert x.is_cuda and x.is_contiguous() and x.dtype == torch.bfloat16 and x.dim() == 2 and x.shape[1] == w.n_cols
+    m = int(x.shape[0])
+    if out is None:
+        out = torch.empty(m, n, dtype=torch.bfloat16, device=x.device)
+    assert out.is_cuda and out.is_contiguous() and out.dtype == torch.bfloat16 and out.shape == (m, n)
+    with torch.cuda.device(x.device):
+        size = lib.sp_fp4_product_workspace(m, n, w.n_cols, int(gated))
+        work = torch.empty(size, dtype=torch.uint8, device=x.device) if size else None
+        _check(lib.sp_fp4_product(x.data_ptr(), m, w.data.data_ptr(), n, w.n_cols, int(gated), out.data_ptr(),
+                                  work.data_ptr() if size else None, size, _raw_stream(x.device)), "sp_fp4_product")
     return out
 
 

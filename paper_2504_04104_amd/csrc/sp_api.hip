@@ -96,6 +96,8 @@ int check_config(const sp_config* c) {
   if (c->d_model % 8 || c->d_ff % 8) return SP_E_UNSUPPORTED;
   if (c->d_head != 64 && c->d_head != 128) return SP_E_UNSUPPORTED;
   if (!(c->rms_eps > 0.f) || !(c->rope_theta > 1.f)) return SP_E_INVALID;
+  if ((c->flags & (SP_FLAG_FP4_KV | SP_FLAG_FP4_WEIGHTS)) && c->dtype != SP_BF16) return SP_E_UNSUPPORTED;
+  if ((c->flags & SP_FLAG_FP4_WEIGHTS) && (c->flags & SP_FLAG_PACKED_WEIGHTS)) return SP_E_INVALID;
   if (c->flags & SP_FLAG_PAGED_KV) {
     // a page holds whole 32-slot attention tiles
     const int pg = c->page_slots;
@@ -105,6 +107,10 @@ int check_config(const sp_config* c) {
   return SP_OK;
 }
 
+inline bool is_fp4_kv(const sp_config& c) { return (c.flags & SP_FLAG_FP4_KV) != 0; }
+// bytes of a (slot, head) row: storage type, or two codes a byte (the scales lie in planes of their own, four bytes a row)
+inline size_t kv_row_bytes(const sp_config& c) { return is_fp4_kv(c) ? (size_t)c.d_head / 2 : (size_t)c.d_head * elt_bytes(c.dtype); }
+inline size_t scale_plane_bytes(const sp_config& c) { return is_fp4_kv(c) ? (size_t)c.kv_slots * 4 : 0; }
 inline bool is_paged(const sp_config& c) { return (c.flags & SP_FLAG_PAGED_KV) != 0; }
 inline size_t page_table_bytes(const sp_config& c) {
   if (!is_paged(c)) return 0;
@@ -124,6 +130,7 @@ static void* g_noalloc_scratch[SP_NOALLOC_MAX_DEVICES];
 struct sp_stage {
   sp_config cfg;
   std::vector<sp_layer_weights> W;
+  std::vector<sp_head_norms> norms;   // empty: the model has none
   sp_buffers buf;
   sp_sizes sizes;
   ReqMeta* d_meta = nullptr;
@@ -149,6 +156,7 @@ struct sp_stage {
   bool fast = false;           // bf16 MFMA kernels in use
   bool f32 = false;            // float32 MFMA kernels in use
   bool packed = false;         // weights are in MFMA fragment order
+  bool fp4 = false;            // weights are in 4 bits
   int* pin_nodes = nullptr;    // pinned host copy of the device-side verification results (sp_tree_prune_verified)
   hipEvent_t rec_ev = nullptr; // done when that copy has arrived
   int n_cu = 256;              // compute units of the device
@@ -314,10 +322,10 @@ int sp_stage_query_sizes(const sp_config* cfg, sp_sizes* out) {
   int rc = check_config(cfg);
   if (rc != SP_OK) return rc;
   if (!out) return SP_E_INVALID;
-  const size_t row = (size_t)cfg->d_head * elt_bytes(cfg->dtype);
+  const size_t row = kv_row_bytes(*cfg);
   out->kv_row_bytes = row;
   out->kv_plane_bytes = (size_t)cfg->kv_slots * row;
-  out->kv_bytes = (size_t)cfg->n_layers * 2 * cfg->n_kv_heads * out->kv_plane_bytes;
+  out->kv_bytes = (size_t)cfg->n_layers * 2 * cfg->n_kv_heads * (out->kv_plane_bytes + scale_plane_bytes(*cfg));
   out->tables_bytes = tables_meta_bytes(*cfg) + align_up((size_t)cfg->max_requests * sizeof(ReqTables)) +
                       page_table_bytes(*cfg);
   out->workspace_bytes = carve(*cfg, nullptr).total;
@@ -356,6 +364,8 @@ int sp_stage_create(const sp_config* cfg, const sp_layer_weights* layers, const 
   s->geom.n_layers = cfg->n_layers;
   s->geom.n_kv_heads = cfg->n_kv_heads;
   s->geom.page_table = nullptr; s->geom.pt_stride = 0; s->geom.pg_shift = 0;
+  s->geom.scale_plane_bytes = scale_plane_bytes(*cfg);
+  s->geom.scales = is_fp4_kv(*cfg) ? s->geom.kv + (size_t)cfg->n_layers * 2 * cfg->n_kv_heads * sz.kv_plane_bytes : nullptr;
   if (is_paged(*cfg)) {
     s->n_pages = (int)(cfg->kv_slots / cfg->page_slots);
     s->d_page_table = (int*)((char*)buffers->tables + tables_meta_bytes(*cfg) +
@@ -388,7 +398,8 @@ int sp_stage_create(const sp_config* cfg, const sp_layer_weights* layers, const 
   }
   s->use_graphs = !(cfg->flags & SP_FLAG_NO_GRAPHS);
   s->packed = (cfg->flags & SP_FLAG_PACKED_WEIGHTS) != 0;
-  if (s->packed && !s->fast) { delete s; return SP_E_UNSUPPORTED; }
+  s->fp4 = (cfg->flags & SP_FLAG_FP4_WEIGHTS) != 0;
+  if ((s->packed || s->fp4) && !s->fast) { delete s; return SP_E_UNSUPPORTED; }
   hipError_t e = sp_launch_tables_clear(s->d_meta, s->d_tables, cfg->max_requests, (hipStream_t)stream);
   if (e != hipSuccess) { delete s; return SP_E_HIP; }
   *out = s;
@@ -424,6 +435,69 @@ int sp_pack_matrix(const void* in, void* out, int32_t n_rows, int32_t n_cols, sp
   if (!in || !out || in == out || n_rows < 1 || n_cols < 1) return SP_E_INVALID;
   if (n_rows % 16 || n_cols % 32) return SP_E_UNSUPPORTED;
   return sp_launch_pack_weights(in, out, n_rows, n_cols, (hipStream_t)stream) == hipSuccess ? SP_OK : SP_E_HIP;
+}
+
+// ---- 4-bit weights --------------------------------------------------------------------------------
+static bool fp4_shape(int64_t n_rows, int64_t n_cols) {
+  return n_rows >= 16 && n_cols >= 32 && n_rows % 16 == 0 && n_cols % 32 == 0 && n_rows <= SP_FP4_MAX_DIM && n_cols <= SP_FP4_MAX_DIM;
+}
+// compute units of the current device
+static int current_cus() {
+  static int known[SP_NOALLOC_MAX_DEVICES];
+  int dev = 0, cus = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= SP_NOALLOC_MAX_DEVICES) return 256;
+  if (known[dev] > 0) return known[dev];
+  if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus < 1) return 256;
+  return known[dev] = cus;
+}
+
+size_t sp_fp4_matrix_bytes(int32_t n_rows, int32_t n_cols) { return fp4_shape(n_rows, n_cols) ? sp_fp4_bytes(n_rows, n_cols) : 0; }
+
+int sp_fp4_pack_matrix(const void* in, void* out, int32_t n_rows, int32_t n_cols, sp_stream stream) {
+  if (!in || !out || in == out || n_rows < 1 || n_cols < 1 || (((uintptr_t)in | (uintptr_t)out) & 15)) return SP_E_INVALID;
+  if (!fp4_shape(n_rows, n_cols)) return SP_E_UNSUPPORTED;
+  return sp_launch_fp4_pack(in, out, n_rows, n_cols, (hipStream_t)stream) == hipSuccess ? SP_OK : SP_E_HIP;
+}
+
+int sp_fp4_unpack_matrix(const void* in, void* out, int32_t n_rows, int32_t n_cols, sp_stream stream) {
+  if (!in || !out || in == out || n_rows < 1 || n_cols < 1 || (((uintptr_t)in | (uintptr_t)out) & 15)) return SP_E_INVALID;
+  if (!fp4_shape(n_rows, n_cols)) return SP_E_UNSUPPORTED;
+  return sp_launch_fp4_unpack(in, out, n_rows, n_cols, (hipStream_t)stream) == hipSuccess ? SP_OK : SP_E_HIP;
+}
+
+int sp_fp4_pack_weights(const sp_config* cfg, const sp_layer_weights* in, const sp_layer_weights* out, sp_stream stream) {
+  int rc = check_config(cfg);
+  if (rc != SP_OK) return rc;
+  if (!in || !out) return SP_E_INVALID;
+  if (cfg->dtype != SP_BF16) return SP_E_UNSUPPORTED;
+  const int d = cfg->d_model, dq = cfg->n_q_heads * cfg->d_head, nqkv = (cfg->n_q_heads + 2 * cfg->n_kv_heads) * cfg->d_head, F = cfg->d_ff;
+  const void* from[4] = {in->wqkv, in->wo, in->wgu, in->wd};
+  const void* to[4] = {out->wqkv, out->wo, out->wgu, out->wd};
+  const int rows[4] = {nqkv, d, 2 * F, d}, cols[4] = {d, dq, d, F};
+  for (int i = 0; i < 4; ++i) {
+    if (!from[i] || !to[i] || from[i] == to[i] || (((uintptr_t)from[i] | (uintptr_t)to[i]) & 15)) return SP_E_INVALID;
+    if (!fp4_shape(rows[i], cols[i])) return SP_E_UNSUPPORTED;
+  }
+  for (int i = 0; i < 4; ++i)
+    if (sp_launch_fp4_pack(from[i], const_cast<void*>(to[i]), rows[i], cols[i], (hipStream_t)stream) != hipSuccess) return SP_E_HIP;
+  return SP_OK;
+}
+
+size_t sp_fp4_product_workspace(int32_t m, int32_t n, int32_t k, int32_t gated) {
+  if (m < 1 || m > SP_FP4_MAX_DIM || (gated != 0 && gated != 1) || !fp4_shape((int64_t)n << gated, k) || n % 16) return 0;
+  return sp_fp4_product_floats(m, n << gated, k, gated != 0, current_cus()) * sizeof(float);
+}
+
+int sp_fp4_product(const void* x, int32_t m, const void* w, int32_t n, int32_t k, int32_t gated, void* out, void* workspace,
+                   size_t workspace_bytes, sp_stream stream) {
+  if (m < 0 || n < 1 || k < 1 || (gated != 0 && gated != 1)) return SP_E_INVALID;
+  if (m > SP_FP4_MAX_DIM || !fp4_shape((int64_t)n << gated, k) || n % 16) return SP_E_UNSUPPORTED;
+  if (m == 0) return SP_OK;
+  if (!x || !w || !out || (((uintptr_t)x | (uintptr_t)w | (uintptr_t)out | (uintptr_t)workspace) & 15)) return SP_E_INVALID;
+  const size_t need = sp_fp4_product_workspace(m, n, k, gated);
+  if (need > 0 && (!workspace || workspace_bytes < need)) return SP_E_CAPACITY;
+  return sp_launch_fp4_product((const bf16_t*)x, w, gated != 0, (bf16_t*)out, (float*)workspace, m, n << gated, k, current_cus(),
+                               (hipStream_t)stream) == hipSuccess ? SP_OK : SP_E_HIP;
 }
 
 int sp_request_init(sp_stage* s, int32_t req, int64_t slot_base, int32_t capacity, int32_t prefix_len,
@@ -588,13 +662,11 @@ int sp_tree_insert(sp_stage* s, int32_t req, int32_t n_new, const int32_t* paren
   return sp_tree_insert_batch(s, 1, &req, &n_new, parents, tokens, probs, first_index_out, stream);
 }
 
-int sp_stage_forward(sp_stage* s, int32_t n_req, const int32_t* req_ids, const int32_t* first_node,
-                     const int32_t* n_nodes, const void* x_in, void* x_out, sp_stream stream) {
+// The rows of a call over nodes [first_node, first_node + n_nodes) of the requests; a node's parent must have been forwarded or
+// be part of the call.
+static int call_rows(sp_stage* s, int32_t n_req, const int32_t* req_ids, const int32_t* first_node, const int32_t* n_nodes, FwdBatch& b) {
   if (!s || !req_ids || !first_node || !n_nodes) return SP_E_INVALID;
   if (n_req < 0 || n_req > SP_MAX_BATCH_REQ) return SP_E_CAPACITY;
-  const sp_config& c = s->cfg;
-  hipStream_t st = (hipStream_t)stream;
-  FwdBatch b;
   b.n_req = 0;
   int rows = 0;
   for (int i = 0; i < n_req; ++i) {
@@ -604,7 +676,7 @@ int sp_stage_forward(sp_stage* s, int32_t n_req, const int32_t* req_ids, const i
     for (int j = 0; j < i; ++j) if (req_ids[j] == req_ids[i]) return SP_E_INVALID;
     if (n_nodes[i] < 0) return SP_E_INVALID;
     if (n_nodes[i] == 0) continue;
-    if (first_node[i] < 0 || first_node[i] + n_nodes[i] > r->T) return SP_E_BAD_NODE;
+    if (first_node[i] < 0 || first_node[i] > r->T || n_nodes[i] > r->T - first_node[i]) return SP_E_BAD_NODE;
     for (int k = first_node[i]; k < first_node[i] + n_nodes[i]; ++k) {
       const int p = r->parent[k];
       if (p >= 0 && !r->fwd[p] && p < first_node[i]) return SP_E_ORDER;
@@ -613,25 +685,25 @@ int sp_stage_forward(sp_stage* s, int32_t n_req, const int32_t* req_ids, const i
     ++b.n_req;
     rows += n_nodes[i];
   }
-  if (rows > c.max_batch_nodes) return SP_E_CAPACITY;
-  if (rows == 0) return SP_OK;
-  if (!x_in || !x_out) return SP_E_INVALID;
   b.n_rows = rows;
-  const int M = rows, d = c.d_model, F = c.d_ff, dh = c.d_head, nq = c.n_q_heads, nkv = c.n_kv_heads;
-  const int dq = nq * dh, nqkv = (nq + 2 * nkv) * dh;
-  const int dt = c.dtype;
-  Workspace& w = s->ws;
-  hipError_t e;
-#define SP_TRY(call) do { e = (call); if (e != hipSuccess) return hip_fail(s, e); } while (0)
+  return rows > s->cfg.max_batch_nodes ? SP_E_CAPACITY : SP_OK;
+}
 
-  AttnPlan plan;
+static void mark_forwarded(sp_stage* s, const FwdBatch& b) {
+  for (int i = 0; i < b.n_req; ++i) {
+    HostReq& r = s->reqs[b.req[i]];
+    for (int k = b.first[i]; k < b.first[i] + b.n[i]; ++k) r.fwd[k] = 1;
+  }
+}
+
+// Which request and node each row belongs to.  Longest cache ranges first (equal ones in the call's order): the attention's
+// workgroups start in this order, and those of short ranges fill the CUs that the long ones leave over (us a layer of the 8B shape
+// behind 512-4096 slots, the call's order / longest first: 32 requests of 8-32 nodes 429.9 / 397.3, 64 of 1-4 256.8 / 244.5, two
+// layers of 638 rows 823 / 780; one round of workgroups, or ranges cut into chunks, level).
+static void plan_segments(const sp_stage* s, const FwdBatch& b, void* x_out, AttnPlan& plan) {
   std::memset(&plan, 0, sizeof(plan));
   plan.n_seg = b.n_req;
   plan.x_out = x_out;
-  // Which request and node each row belongs to.  Longest cache ranges first (equal ones in the call's order): the attention's
-  // workgroups start in this order, and those of short ranges fill the CUs that the long ones leave over (us a layer of the 8B shape
-  // behind 512-4096 slots, the call's order / longest first: 32 requests of 8-32 nodes 429.9 / 397.3, 64 of 1-4 256.8 / 244.5, two
-  // layers of 638 rows 823 / 780; one round of workgroups, or ranges cut into chunks, level).
   short order[SP_BATCH];
   for (int i = 0; i < b.n_req; ++i) {
     const HostReq& r = s->reqs[b.req[i]];
@@ -646,10 +718,34 @@ int sp_stage_forward(sp_stage* s, int32_t n_req, const int32_t* req_ids, const i
     plan.seg_first[k] = b.first[i]; plan.seg_P[k] = r.P; plan.seg_T[k] = r.T; plan.seg_base[k] = r.base;
     plan.seg_chunks[k] = 1;
   }
-  if (s->fast && !attn_split(plan, nq, nkv, s->n_cu, w.attn_units)) return SP_E_CAPACITY;
+}
 
-  const size_t strideD = (size_t)M * d, strideQ = (size_t)M * nqkv;
-  const bool few = s->fast && sp_few_takes(M, d, dq, F, s->packed, s->n_cu);
+int sp_stage_forward(sp_stage* s, int32_t n_req, const int32_t* req_ids, const int32_t* first_node,
+                     const int32_t* n_nodes, const void* x_in, void* x_out, sp_stream stream) {
+  FwdBatch b;
+  const int rc = call_rows(s, n_req, req_ids, first_node, n_nodes, b);
+  if (rc != SP_OK) return rc;
+  const sp_config& c = s->cfg;
+  hipStream_t st = (hipStream_t)stream;
+  if (b.n_rows == 0) return SP_OK;
+  if (!x_in || !x_out) return SP_E_INVALID;
+  const int M = b.n_rows, d = c.d_model, F = c.d_ff, dh = c.d_head, nq = c.n_q_heads, nkv = c.n_kv_heads;
+  const int dq = nq * dh, nqkv = (nq + 2 * nkv) * dh;
+  const int dt = c.dtype;
+  Workspace& w = s->ws;
+  hipError_t e;
+#define SP_TRY(call) do { e = (call); if (e != hipSuccess) return hip_fail(s, e); } while (0)
+
+  AttnPlan plan;
+  plan_segments(s, b, x_out, plan);
+  const bool kv4 = s->geom.scales != nullptr, normed = !s->norms.empty();
+  if ((s->fast || kv4) && !attn_split(plan, nq, nkv, s->n_cu, w.attn_units)) return SP_E_CAPACITY;
+
+  const size_t strideD = (size_t)M * d;
+  // Complete projections, and in float32 the joined one, rotate a few columns of a head at a time: heads that are normed, or held
+  // in groups of 32 columns, take the way over partial sums and a launch that has whole heads.
+  const bool whole_heads = kv4 || normed;
+  const bool few = s->fast && !whole_heads && !s->fp4 && sp_few_takes(M, d, dq, F, s->packed, s->n_cu);
   // Activations between the products in fragment order, but few rows row-major where no product takes them by
   // direct-to-LDS loads; and in the many-row kernel beside row-major weights.  Complete projections: a k step is M pieces of
   // 64 bytes row-major and 512 bytes for every eight rows in fragment order, which moves 1.75 times as fast per byte: row-major
@@ -658,11 +754,13 @@ int sp_stage_forward(sp_stage* s, int32_t n_req, const int32_t* req_ids, const i
   // Split products up to eight rows (5120 and 4096 wide, two layers, 6 rows 247.4 / 203.4 us in fragment order, 246.1 / 199.9
   // row-major).
   const bool few_lines = !few ? M <= 8 : s->packed ? 7 * M < 32 * ((M + 7) / 8) : M <= 4;
-  const bool frag = s->fast && !(few_lines && (s->packed || (few && !sp_gemm_mid_takes_gateup(M, F, d, false, s->n_cu)))) &&
-                    (s->packed || M <= 160);
+  const bool frag = s->fp4 ? M > 8
+                           : s->fast && !(few_lines && (s->packed || (few && !sp_gemm_mid_takes_gateup(M, F, d, false, s->n_cu)))) &&
+                                 (s->packed || M <= 160);
   // projections: few rows stream the weights (HBM-bound); many rows use the register-blocked kernel
-  const bool wide = s->fast && M > 128 && nqkv % 256 == 0 && d % 256 == 0 && F % 128 == 0 && dq % 128 == 0;
+  const bool wide = s->fast && !s->fp4 && M > 128 && nqkv % 256 == 0 && d % 256 == 0 && F % 128 == 0 && dq % 128 == 0;
   auto gemm = [&](const void* X, const void* Wm, int N_, int K_, int* S_, bool resident = false) -> hipError_t {
+    if (s->fp4) return sp_launch_fp4_parts((const bf16_t*)X, frag, Wm, w.part, M, N_, K_, s->n_cu, w.part_floats, S_, st);
     if (sp_gemm_mid_takes(M, N_, K_, s->packed, s->n_cu))
       return sp_launch_gemm_mid((const bf16_t*)X, (const bf16_t*)Wm, s->packed, w.part, M, N_, K_, s->n_cu, 16,
                                 w.part_floats, S_, st, resident);
@@ -708,7 +806,15 @@ int sp_stage_forward(sp_stage* s, int32_t n_req, const int32_t* req_ids, const i
   };
   // float32: five launches a layer (the same products between norms, rotation, append, residual and write-out as launches
   // of their own were eight, 2 layers of d = 256 at 16 nodes 70.1 -> 60.7 us a call), seven where QKV has many workgroups
-  const bool qkv_joined = s->f32 && sp_qkv_f32_joined(M, nqkv, s->n_cu);
+  const bool qkv_joined = s->f32 && !whole_heads && sp_qkv_f32_joined(M, nqkv, s->n_cu);
+  // sums of the QKV projection to rotated queries and cache rows
+  auto rope_append = [&](int l, int S) -> hipError_t {
+    ProfScope p(s, SP_K_ROPE_KV, st);
+    if (whole_heads)
+      return sp_launch_append_parts(dt, w.part, S, (size_t)M * nqkv, w.rows, w.cs, normed ? s->norms[l].q : nullptr,
+                                    normed ? s->norms[l].k : nullptr, c.rms_eps, w.qbuf, s->geom, l, M, nq, nkv, dh, st);
+    return sp_launch_rope_kv(dt, w.part, S, (size_t)M * nqkv, w.rows, w.cs, w.qbuf, s->geom, l, M, nq, nkv, dh, st);
+  };
   auto run_layers_f32 = [&]() -> hipError_t {
     for (int l = 0; l < c.n_layers; ++l) {
       const sp_layer_weights& L = s->W[l];
@@ -723,8 +829,7 @@ int sp_stage_forward(sp_stage* s, int32_t n_req, const int32_t* req_ids, const i
         }
         { ProfScope p(s, SP_K_GEMM_QKV, st);
           SP_STEP(sp_launch_gemm_f32((const float*)w.xn, (const float*)L.wqkv, w.part, M, nqkv, d, st)); }
-        { ProfScope p(s, SP_K_ROPE_KV, st);
-          SP_STEP(sp_launch_rope_kv(dt, w.part, 1, strideQ, w.rows, w.cs, w.qbuf, s->geom, l, M, nq, nkv, dh, st)); }
+        SP_STEP(rope_append(l, 1));
       }
       { ProfScope p(s, SP_K_ATTENTION, st);
         SP_STEP(sp_launch_attn_f32((const float*)w.qbuf, w.rows, s->d_tables, s->geom, l, (float*)w.attn, M, nq, nkv, dh, st)); }
@@ -752,9 +857,12 @@ int sp_stage_forward(sp_stage* s, int32_t n_req, const int32_t* req_ids, const i
       { ProfScope p(s, SP_K_GEMM_QKV, st);
         if (s->fast) SP_STEP(gemm(w.xn, L.wqkv, nqkv, d, &S));
         else SP_STEP(sp_launch_gemm_simple(dt, w.xn, L.wqkv, w.part, M, nqkv, d, st)); }
-      { ProfScope p(s, SP_K_ROPE_KV, st);
-        SP_STEP(sp_launch_rope_kv(dt, w.part, S, strideQ, w.rows, w.cs, w.qbuf, s->geom, l, M, nq, nkv, dh, st)); }
-      if (s->fast) {
+      SP_STEP(rope_append(l, S));
+      if (kv4) {
+        ProfScope p(s, SP_K_ATTENTION, st);
+        SP_STEP(sp_launch_attn_fp4((const bf16_t*)w.qbuf, s->d_tables, s->geom, l, plan, w.plan, w.attn_part, (bf16_t*)w.attn, frag,
+                                   M, nq, nkv, dh, st));
+      } else if (s->fast) {
         ProfScope p(s, SP_K_ATTENTION, st);
         SP_STEP(sp_launch_attn_bf16((const bf16_t*)w.qbuf, s->d_tables, s->geom, l, plan, w.plan, w.attn_part,
                                     (bf16_t*)w.attn, frag, M, nq, nkv, dh, st));
@@ -770,7 +878,8 @@ int sp_stage_forward(sp_stage* s, int32_t n_req, const int32_t* req_ids, const i
         SP_STEP(sp_launch_add_norm(dt, w.h, w.part, S, strideD, L.norm2, w.xn, frag, M, d, c.rms_eps, st)); }
       { ProfScope p(s, SP_K_GEMM_GATEUP, st);
         if (s->fast) {
-          if (sp_gemm_mid_takes_gateup(M, F, d, s->packed, s->n_cu)) SP_STEP(sp_launch_gemm_mid_gateup((const bf16_t*)w.xn, (const bf16_t*)L.wgu, s->packed, (bf16_t*)w.act, M, F, d, s->n_cu, nullptr, 0.f, st));
+          if (s->fp4) SP_STEP(sp_launch_fp4_gateup((const bf16_t*)w.xn, frag, L.wgu, (bf16_t*)w.act, M, F, d, s->n_cu, st));
+          else if (sp_gemm_mid_takes_gateup(M, F, d, s->packed, s->n_cu)) SP_STEP(sp_launch_gemm_mid_gateup((const bf16_t*)w.xn, (const bf16_t*)L.wgu, s->packed, (bf16_t*)w.act, M, F, d, s->n_cu, nullptr, 0.f, st));
           else if (wide) SP_STEP(sp_launch_gemm_wide_gateup((const bf16_t*)w.xn, frag, (const bf16_t*)L.wgu, s->packed, (bf16_t*)w.act, M, F, d, s->n_cu, st));
           else SP_STEP(sp_launch_gemm_gateup_bf16((const bf16_t*)w.xn, frag, (const bf16_t*)L.wgu, s->packed, (bf16_t*)w.act, M, F, d, s->n_cu, nullptr, 0.f, st));
         } else {
@@ -862,11 +971,102 @@ int sp_stage_forward(sp_stage* s, int32_t n_req, const int32_t* req_ids, const i
   }
   if (!done) SP_TRY(run_layers());
 #undef SP_TRY
-  for (int i = 0; i < b.n_req; ++i) {
-    HostReq& r = s->reqs[b.req[i]];
-    for (int k = b.first[i]; k < b.first[i] + b.n[i]; ++k) r.fwd[k] = 1;
-  }
+  mark_forwarded(s, b);
   return SP_OK;
+}
+
+// ---- a layer's attention piece by piece ---------------------------------------------------------
+int sp_stage_set_head_norms(sp_stage* s, const sp_head_norms* layers) {
+  if (!s) return SP_E_INVALID;
+  if (layers)
+    for (int l = 0; l < s->cfg.n_layers; ++l) {
+      if (!layers[l].q || !layers[l].k) return SP_E_INVALID;
+      if (((uintptr_t)layers[l].q | (uintptr_t)layers[l].k) & 15) return SP_E_INVALID;
+    }
+  if (layers) s->norms.assign(layers, layers + s->cfg.n_layers);
+  else s->norms.clear();
+  // what was captured does not know these pointers
+  for (auto& g : s->graphs) if (g.exec) (void)hipGraphExecDestroy(g.exec);
+  s->graphs.clear();
+  return SP_OK;
+}
+
+int sp_stage_append(sp_stage* s, int32_t layer, int32_t n_req, const int32_t* req_ids, const int32_t* first_node, const int32_t* n_nodes,
+                    const void* qkv, void* q_out, sp_stream stream) {
+  FwdBatch b;
+  const int rc = call_rows(s, n_req, req_ids, first_node, n_nodes, b);
+  if (rc != SP_OK) return rc;
+  const sp_config& c = s->cfg;
+  if (layer < 0 || layer >= c.n_layers) return SP_E_INVALID;
+  if (b.n_rows == 0) return SP_OK;
+  if (!qkv || !q_out || (((uintptr_t)qkv | (uintptr_t)q_out) & 15)) return SP_E_INVALID;
+  const bool normed = !s->norms.empty();
+  { ProfScope p(s, SP_K_ROPE_KV, (hipStream_t)stream);
+    const hipError_t e = sp_launch_append_rows(c.dtype, qkv, b, s->d_meta, s->d_tables, std::log2((double)c.rope_theta),
+                                               normed ? s->norms[layer].q : nullptr, normed ? s->norms[layer].k : nullptr, c.rms_eps,
+                                               q_out, s->geom, layer, c.n_q_heads, c.n_kv_heads, c.d_head, (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(s, e); }
+  if (layer == c.n_layers - 1) mark_forwarded(s, b);
+  return SP_OK;
+}
+
+int sp_stage_attention(sp_stage* s, int32_t layer, int32_t n_req, const int32_t* req_ids, const int32_t* first_node,
+                       const int32_t* n_nodes, const void* q, void* out, sp_stream stream) {
+  FwdBatch b;
+  const int rc = call_rows(s, n_req, req_ids, first_node, n_nodes, b);
+  if (rc != SP_OK) return rc;
+  const sp_config& c = s->cfg;
+  if (layer < 0 || layer >= c.n_layers) return SP_E_INVALID;
+  if (b.n_rows == 0) return SP_OK;
+  if (!q || !out || q == out || (((uintptr_t)q | (uintptr_t)out) & 15)) return SP_E_INVALID;
+  hipStream_t st = (hipStream_t)stream;
+  const Workspace& w = s->ws;
+  const int M = b.n_rows, nq = c.n_q_heads, nkv = c.n_kv_heads, dh = c.d_head;
+  AttnPlan plan;
+  plan_segments(s, b, nullptr, plan);
+  const bool kv4 = s->geom.scales != nullptr;
+  if ((s->fast || kv4) && !attn_split(plan, nq, nkv, s->n_cu, w.attn_units)) return SP_E_CAPACITY;
+  ProfScope p(s, SP_K_ATTENTION, st);
+  hipError_t e;
+  if (kv4) {
+    e = sp_launch_attn_fp4((const bf16_t*)q, s->d_tables, s->geom, layer, plan, nullptr, w.attn_part, (bf16_t*)out, false, M, nq, nkv,
+                           dh, st);
+    return e == hipSuccess ? SP_OK : hip_fail(s, e);
+  }
+  // the kernels over a cache in the storage type find the call's rows in the workspace
+  if ((e = sp_launch_call_rows(plan, w.plan, s->d_meta, s->d_tables, w.rows, M, st)) != hipSuccess) return hip_fail(s, e);
+  if (s->fast) e = sp_launch_attn_bf16((const bf16_t*)q, s->d_tables, s->geom, layer, plan, w.plan, w.attn_part, (bf16_t*)out, false, M, nq, nkv, dh, st);
+  else if (s->f32) e = sp_launch_attn_f32((const float*)q, w.rows, s->d_tables, s->geom, layer, (float*)out, M, nq, nkv, dh, st);
+  else e = sp_launch_attn_simple(c.dtype, q, w.rows, s->d_tables, s->geom, layer, out, M, nq, nkv, dh, st);
+  return e == hipSuccess ? SP_OK : hip_fail(s, e);
+}
+
+static int check_slots(sp_stage* s, int32_t req, int32_t layer, int32_t first_slot, int32_t n, const void* k, const void* v) {
+  if (!s) return SP_E_INVALID;
+  HostReq* r = get_req(s, req);
+  if (!r) return SP_E_BAD_REQ;
+  if (r->pending) return SP_E_PENDING;
+  if (layer < 0 || layer >= s->cfg.n_layers || first_slot < 0 || n < 0) return SP_E_INVALID;
+  if ((long long)first_slot + n > r->P + r->T) return SP_E_CAPACITY;
+  if (n > 0 && (!k || !v || (((uintptr_t)k | (uintptr_t)v) & 15))) return SP_E_INVALID;
+  return SP_OK;
+}
+
+int sp_kv_store(sp_stage* s, int32_t req, int32_t layer, int32_t first_slot, int32_t n, const void* k, const void* v, sp_stream stream) {
+  const int rc = check_slots(s, req, layer, first_slot, n, k, v);
+  if (rc != SP_OK || n == 0) return rc;
+  const hipError_t e = sp_launch_kv_store(s->cfg.dtype, s->geom, req, s->reqs[req].base, layer, first_slot, n, k, v, s->cfg.n_kv_heads,
+                                          s->cfg.d_head, (hipStream_t)stream);
+  return e == hipSuccess ? SP_OK : hip_fail(s, e);
+}
+
+int sp_kv_load(sp_stage* s, int32_t req, int32_t layer, int32_t first_slot, int32_t n, void* k, void* v, sp_stream stream) {
+  const int rc = check_slots(s, req, layer, first_slot, n, k, v);
+  if (rc != SP_OK || n == 0) return rc;
+  if (k == v) return SP_E_INVALID;
+  const hipError_t e = sp_launch_kv_load(s->cfg.dtype, s->geom, req, s->reqs[req].base, layer, first_slot, n, k, v, s->cfg.n_kv_heads,
+                                         s->cfg.d_head, (hipStream_t)stream);
+  return e == hipSuccess ? SP_OK : hip_fail(s, e);
 }
 
 int sp_tree_prune_batch(sp_stage* s, int32_t n, const int32_t* req_ids, const int32_t* modes, const int32_t* nodes,

@@ -25,7 +25,7 @@
 // 4096 slots, 43.7 us alone: 36.9 without the global loads, 23.6 without them and the LDS stores), and the V fragments came in
 // 32-bit reads with a permutation each.  Direct-to-LDS loads and transposing reads: 48.1 -> 38.0 us in the step, one request of
 // a few rows behind 32768 slots 27.3 -> 26.1 us.
-#include "sp_launch.h"
+#include "sp_attn.h"
 
 #define DH 128
 #define TILE_BYTES (32 * 256)   // 32 slots of K or V
@@ -41,22 +41,6 @@ struct AttnArgs {
   const AttnPlan* plan;     // device copy of the call's plan (written by the kernel that opens the forward)
 };
 
-// Online softmax of a wave over QT tiles of 16 query rows.  mrun is the running maximum of the raw scores q.k; negm =
-// -mrun*sc (0 while mrun is -inf), so that exp2(fma(s, sc, negm)) is the softmax weight.
-template <int QT>
-struct AttnState {
-  f32x4_t o[QT][8];
-  float mrun[QT], lrun[QT], negm[QT];
-  __device__ __forceinline__ void init() {
-#pragma unroll
-    for (int t = 0; t < QT; ++t) {
-      mrun[t] = -INFINITY; lrun[t] = 0.f; negm[t] = 0.f;
-#pragma unroll
-      for (int d = 0; d < 8; ++d) o[t][d] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-    }
-  }
-};
-#define ATTN_SC (0.08838834764831845f * 1.4426950408889634f)   // 1/sqrt(128) * log2(e)
 
 // A tile's rows lie in LDS as they do in memory, 256 bytes each, but that the 16-byte units of a row are exchanged by the row's
 // number (unit u is at place u ^ unit_swap(row)): the direct-to-LDS loads leave no room for padding.  Sixteen rows' fragments
@@ -84,69 +68,8 @@ __device__ __forceinline__ void attn_scores(f32x4_t (&sacc)[QT][2], const u32x4_
     }
 }
 
-// Scores of the tile with first slot s0, of a run that ends at w1, to weights (bf16 pairs, in the order of sacc's slots).
-template <int QT>
-__device__ __forceinline__ void attn_softmax(AttnState<QT>& st, const f32x4_t (&sacc)[QT][2], uint32_t (&pb)[QT][4],
-                                             const unsigned long long (&anc)[QT][SP_W], int s0, int w1, int P, int span, int kg) {
-  const float sc = ATTN_SC;
-  const bool tail = s0 + 32 > P || s0 + 32 > w1;   // tile touches the tree region or the run's end
-#pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    float sv[8];
-#pragma unroll
-    for (int t2 = 0; t2 < 2; ++t2)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) sv[t2 * 4 + i] = sacc[t][t2][i];
-    if (tail) {
-      // bits [n0, n0+64) of the row's 256-bit ancestor mask, n0 = first tree index of the tile
-      const int n0 = s0 - P;
-      unsigned long long win = 0ull;
-#pragma unroll
-      for (int w = 0; w < SP_W; ++w) {
-        const int sh = w * 64 - n0;
-        if (sh > -64 && sh < 64) win |= sh >= 0 ? (anc[t][w] << sh) : (anc[t][w] >> (-sh));
-      }
-      const int lim = w1 - s0, pfx = P - s0, tl = span - s0;   // offsets below: in run / committed / live
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int off = (j >> 2) * 16 + kg * 4 + (j & 3);
-        const bool vis = (off < lim) & ((off < pfx) | ((off < tl) & (bool)((win >> off) & 1ull)));
-        sv[j] = vis ? sv[j] : -INFINITY;
-      }
-    }
-    float mx = fmaxf(fmaxf(fmaxf(sv[0], sv[1]), fmaxf(sv[2], sv[3])), fmaxf(fmaxf(sv[4], sv[5]), fmaxf(sv[6], sv[7])));
-    // The running maximum only has to bound the scores, so it is raised (and the
-    // accumulators rescaled) only when some lane of the wave sees a larger score.
-    if (__builtin_amdgcn_ballot_w64(mx > st.mrun[t])) {
-      mx = quad_rows_max(mx);
-      const float mnew = fmaxf(st.mrun[t], mx);
-      const float alpha = (mnew == -INFINITY) ? 1.f : __builtin_amdgcn_exp2f((st.mrun[t] - mnew) * sc);  // 0 from -inf
-      st.lrun[t] *= alpha;
-#pragma unroll
-      for (int d = 0; d < 8; ++d) st.o[t][d] *= alpha;
-      st.mrun[t] = mnew;
-      st.negm[t] = (mnew == -INFINITY) ? 0.f : -mnew * sc;
-    }
-    float pv[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) pv[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(sv[j], sc, st.negm[t]));
-    st.lrun[t] += ((pv[0] + pv[1]) + (pv[2] + pv[3])) + ((pv[4] + pv[5]) + (pv[6] + pv[7]));
-#pragma unroll
-    for (int j = 0; j < 4; ++j) pb[t][j] = pack_bf16x2(pv[2 * j], pv[2 * j + 1]);
-  }
-
-}
-
 // O^T += V^T P^T; va: the lane's places for the transposing reads.  Sixteen lanes read four slots x 16 columns, lane 4c + x of
 // them gets the four slots of column G*32 + 8c + 4e + x, and so a lane's products of e = 0 and 1 are eight columns in a row.
-typedef __attribute__((ext_vector_type(4))) short s16x4_t;
-__device__ __forceinline__ uint2 read_transposed(const char* p) {
-#ifdef __HIP_DEVICE_COMPILE__
-  return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(p)));
-#else
-  return uint2{0u, 0u};
-#endif
-}
 template <int QT>
 __device__ __forceinline__ void attn_pv(AttnState<QT>& st, const uint32_t (&pb)[QT][4], const char* vt, const int (&va)[4]) {
 #pragma unroll
@@ -385,7 +308,7 @@ __global__ void __launch_bounds__(64 * AW) k_attn_bf16(AttnArgs a) {
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
     st.lrun[t] = quad_rows_sum(st.lrun[t]);
-    st.mrun[t] = st.mrun[t] * ATTN_SC;              // to the log2 domain (-inf stays -inf)
+    st.mrun[t] = st.mrun[t] * attn_scale<8>();              // to the log2 domain (-inf stays -inf)
     if (kg == 0) s_m[wave][t * 16 + l15] = st.mrun[t];
   }
   __syncthreads();                       // every wave is done with its tiles; maxima are posted
@@ -444,82 +367,7 @@ __global__ void __launch_bounds__(64 * AW) k_attn_bf16(AttnArgs a) {
   }
 }
 
-// One wave per (row, query head) of the requests that were cut into several chunks: combine the
-// chunk partials (log2-domain maxima).  Lane c first takes chunk c's (max, sum) and turns them into
-// the chunk's weight; the outputs are then accumulated chunk by chunk, two columns per lane.
-__global__ void __launch_bounds__(256) k_attn_merge(AttnArgs a, int M) {
-  const AttnPlan& plan = *a.plan;
-  int sg_chunks = plan.seg_chunks[0], sg_rows = plan.seg_rows[0], sg_unit0 = plan.seg_unit0[0], sg_row0 = plan.seg_row0[0];
-  const int n_seg = plan.n_seg;
-  const float* part_ml = a.part_o + (size_t)plan.units_total * DH;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  // a workgroup takes four rows of a head; the two that fill the output's 128-byte lines (eight rows in fragment order)
-  // run on the same XCD, whose L2 puts the lines together
-  const int pair = (blockIdx.x >> 4) * 8 + (blockIdx.x & 7), row8 = pair / a.n_q, head = pair - row8 * a.n_q;
-  const int row = row8 * 8 + ((blockIdx.x >> 3) & 1) * 4 + wave;
-  if (row >= M) return;
-  if (n_seg > 1) {                       // each lane looks at a segment
-    const int first = plan.seg_row0[lane], seg = __ffsll((unsigned long long)__builtin_amdgcn_ballot_w64(lane < n_seg && row >= first && row < first + plan.seg_rows[lane])) - 1;
-    sg_chunks = plan.seg_chunks[seg]; sg_rows = plan.seg_rows[seg]; sg_unit0 = plan.seg_unit0[seg]; sg_row0 = plan.seg_row0[seg];
-  }
-  const int chunks = sg_chunks, seg_rows = sg_rows;
-  if (chunks == 1) return;               // written directly by the attention kernel
-  const size_t stride = (size_t)seg_rows * a.n_q;
-  const size_t u0 = (size_t)sg_unit0 + (size_t)(row - sg_row0) * a.n_q + head;
-  float acc0 = 0.f, acc1 = 0.f, lsum = 0.f, mx = -INFINITY;
-  for (int c0 = 0; c0 < chunks; c0 += 64) {        // blocks of 64 chunks (one is the rule)
-    const int c = c0 + lane;
-    float m = -INFINITY, l = 0.f;
-    if (c < chunks) {
-      const float2 ml = *reinterpret_cast<const float2*>(part_ml + (u0 + c * stride) * 2);
-      m = ml.x; l = ml.y;
-    }
-    const float bm = wave_max(m);
-    const float nmx = fmaxf(mx, bm);
-    if (nmx == -INFINITY) continue;
-    const float resc = (mx == -INFINITY) ? 0.f : __builtin_amdgcn_exp2f(mx - nmx);
-    acc0 *= resc; acc1 *= resc; lsum *= resc;
-    mx = nmx;
-    const float wgt = (m == -INFINITY) ? 0.f : __builtin_amdgcn_exp2f(m - mx);
-    lsum += wave_sum(wgt * l);
-    const int nb = min(64, chunks - c0);
-    int j = 0;
-    // sixteen chunks' partial rows in flight at a time: the loop is a chain of memory round trips otherwise
-    for (; j + 16 <= nb; j += 16) {
-      float o0[16], o1[16];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float* po = a.part_o + (u0 + (size_t)(c0 + j + i) * stride) * DH;
-        const float2 v = *reinterpret_cast<const float2*>(po + 2 * lane);
-        o0[i] = v.x; o1[i] = v.y;
-      }
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float w1 = __shfl(wgt, j + i, 64);
-        acc0 += w1 * o0[i]; acc1 += w1 * o1[i];
-      }
-    }
-    for (; j + 4 <= nb; j += 4) {
-      float w4[4], o0[4], o1[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        w4[i] = __shfl(wgt, j + i, 64);
-        const float* po = a.part_o + (u0 + (size_t)(c0 + j + i) * stride) * DH;
-        const float2 v = *reinterpret_cast<const float2*>(po + 2 * lane);
-        o0[i] = v.x; o1[i] = v.y;
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) { acc0 += w4[i] * o0[i]; acc1 += w4[i] * o1[i]; }
-    }
-    for (; j < nb; ++j) {
-      const float w1 = __shfl(wgt, j, 64);
-      const float2 v = *reinterpret_cast<const float2*>(a.part_o + (u0 + (size_t)(c0 + j) * stride) * DH + 2 * lane);
-      acc0 += w1 * v.x; acc1 += w1 * v.y;
-    }
-  }
-  const float inv = 1.f / lsum;
-  *reinterpret_cast<uint32_t*>(a.out + row_at(a.frag, row, head * DH + 2 * lane, a.n_q * DH)) = pack_bf16x2(acc0 * inv, acc1 * inv);
-}
+__global__ void __launch_bounds__(256) k_attn_merge(AttnArgs a, int M) { attn_merge<DH>(*a.plan, a.part_o, a.out, a.frag, a.n_q, M); }
 
 hipError_t sp_launch_attn_bf16(const bf16_t* q, const ReqTables* tables, KvGeom g, int layer, const AttnPlan& plan,
                                const AttnPlan* plan_dev, float* part, bf16_t* out, bool frag, int M,

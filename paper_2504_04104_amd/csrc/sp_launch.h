@@ -15,6 +15,10 @@ struct KvGeom {
   int* page_table;
   int pt_stride;
   int pg_shift;
+  // A cache in 4 bits: rows are d_head / 2 bytes of codes, and four bytes of scales per row lie in planes of their own, in the
+  // order of the code planes.  Null: the cache holds the storage type.
+  char* scales;
+  size_t scale_plane_bytes;
 };
 
 // Physical slot of a request's logical slot (base is the request's first slot when contiguous, 0 when paged).
@@ -164,3 +168,37 @@ hipError_t sp_launch_attn_simple(int dtype, const void* q, const RowInfo* rows, 
 hipError_t sp_launch_attn_bf16(const bf16_t* q, const ReqTables* tables, KvGeom g, int layer, const AttnPlan& plan,
                                const AttnPlan* plan_dev, float* part /*workspace*/, bf16_t* out, bool frag, int M,
                                int n_q, int n_kv, int d_head, hipStream_t st);
+
+// ---- 4-bit storage (sp_fp4.h) ------------------------------------------------------
+// tree attention over a cache in 4 bits, d_head 128 or 64; plan_dev null: the plan travels with the launch
+hipError_t sp_launch_attn_fp4(const bf16_t* q, const ReqTables* tables, KvGeom g, int layer, const AttnPlan& plan,
+                              const AttnPlan* plan_dev /*nullable*/, float* part /*workspace*/, bf16_t* out, bool frag, int M,
+                              int n_q, int n_kv, int d_head, hipStream_t st);
+// Head norms (gains nullable: none), rotation and cache append (sp_heads.hip) of QKV rows; into whichever cache g describes.
+// _parts: float32 sums of slices, with the forward call's row descriptors; _rows: rows in the storage type
+hipError_t sp_launch_append_parts(int dtype, const float* part, int S, size_t part_stride, const RowInfo* rows, const float* cs,
+                                  const void* gain_q, const void* gain_k, float eps, void* qbuf, KvGeom g, int layer, int M,
+                                  int n_q, int n_kv, int d_head, hipStream_t st);
+hipError_t sp_launch_append_rows(int dtype, const void* x, const FwdBatch& b, const ReqMeta* meta, const ReqTables* tables,
+                                 double log2_theta, const void* gain_q, const void* gain_k, float eps, void* q, KvGeom g, int layer,
+                                 int n_q, int n_kv, int d_head, hipStream_t st);
+// K and V rows [n][n_kv][d_head] of logical slots first .. first + n - 1 into the cache, and out of it
+hipError_t sp_launch_kv_store(int dtype, KvGeom g, int req, long long base, int layer, int first, int n, const void* k, const void* v,
+                              int n_kv, int d_head, hipStream_t st);
+hipError_t sp_launch_kv_load(int dtype, KvGeom g, int req, long long base, int layer, int first, int n, void* k, void* v, int n_kv,
+                             int d_head, hipStream_t st);
+// Matrices of 4-bit weights: N % 16 == 0, K % 32 == 0
+size_t sp_fp4_bytes(int N, int K);
+hipError_t sp_launch_fp4_pack(const void* in, void* out, int N, int K, hipStream_t st);
+hipError_t sp_launch_fp4_unpack(const void* in, void* out, int N, int K, hipStream_t st);
+// out: partial sums [S][M][N] as sp_launch_gemm_bf16 leaves them.  frag: X (and act) in fragment order, K % 256 == 0 then
+hipError_t sp_launch_fp4_parts(const bf16_t* X, bool frag, const void* W, float* out, int M, int N, int K, int n_cu, size_t part_floats,
+                               int* S_out, hipStream_t st);
+hipError_t sp_launch_fp4_gateup(const bf16_t* X, bool frag, const void* W, bf16_t* act, int M, int F, int K, int n_cu, hipStream_t st);
+// out: bf16 [M][N], or gated [M][N / 2]; part: as many floats as sp_fp4_product_floats says
+size_t sp_fp4_product_floats(int M, int N, int K, bool gated, int n_cu);
+hipError_t sp_launch_fp4_product(const bf16_t* X, const void* W, bool gated, bf16_t* out, float* part, int M, int N, int K, int n_cu,
+                                 hipStream_t st);
+// row descriptors of a call's rows, and its plan, to device memory
+hipError_t sp_launch_call_rows(const AttnPlan& plan, AttnPlan* plan_dev, const ReqMeta* meta, const ReqTables* tables, RowInfo* rows,
+                               int M, hipStream_t st);

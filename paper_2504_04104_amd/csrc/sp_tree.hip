@@ -55,15 +55,18 @@ __global__ void __launch_bounds__(SP_T) k_tree_insert(ReqMeta* meta, ReqTables* 
   if (blockIdx.x > 0) {
     char* plane = g.kv + (size_t)(blockIdx.x - 1) * g.plane_bytes;
     const int u16 = g.row_bytes >> 4;
-    const int n16 = n_new * u16;
+    // (a cache in 4 bits: one unit more per row, its scales)
+    const int per = g.scales ? u16 + 1 : u16;
+    const int n16 = n_new * per;
     for (int i = threadIdx.x; i < n16; i += blockDim.x) {
-      const int row = i / u16, u = i - row * u16;
+      const int row = i / per, u = i - row * per;
       const int lslot = (int)a.first_slot[item] + row;        // (includes the base of a contiguous request)
       const int fresh = (lslot >> g.pg_shift) - a.pg_first[item];
       const size_t slot = fresh >= 0 && fresh < a.pg_n[item]  // a page that this launch is about to enter into the table
                               ? ((size_t)a.page[a.pg_at[item] + fresh] << g.pg_shift) | (size_t)(lslot & ((1 << g.pg_shift) - 1))
                               : sp_phys_slot(g, req, 0, lslot);
-      reinterpret_cast<uint4*>(plane + slot * g.row_bytes)[u] = make_uint4(0u, 0u, 0u, 0u);
+      if (u < u16) reinterpret_cast<uint4*>(plane + slot * g.row_bytes)[u] = make_uint4(0u, 0u, 0u, 0u);
+      else *reinterpret_cast<uint32_t*>(g.scales + (size_t)(blockIdx.x - 1) * g.scale_plane_bytes + slot * 4) = 0u;
     }
     return;
   }
@@ -287,6 +290,18 @@ __global__ void __launch_bounds__(256) k_kv_compact(const ReqMeta* meta, const R
   __syncthreads();
   if (first >= n_keep) return;
   const size_t plane = blockIdx.x;      // (layer*2 + kv) * n_kv_heads + head
+  if (g.scales) {
+    // the scales of a cache in 4 bits: a thread has a row, every row is read before the first is written
+    static_assert(SP_T <= 256, "a row per thread");
+    uint32_t* sc = reinterpret_cast<uint32_t*>(g.scales + plane * g.scale_plane_bytes);
+    const long long at = g.page_table ? 0 : meta[req].base + t.pend_P_old;
+    const int dst = threadIdx.x;
+    const bool mv = dst >= first && dst < n_keep;
+    uint32_t v = 0u;
+    if (mv) v = sc[g.page_table ? (long long)s_phys[s_src[dst]] : at + s_src[dst]];
+    __syncthreads();
+    if (mv) sc[g.page_table ? (long long)s_phys[dst] : at + dst] = v;
+  }
   if (g.page_table) {
     gather_inplace<16>(g.kv + plane * g.plane_bytes, (size_t)g.row_bytes, g.row_bytes, first, n_keep, s_src, s_phys);
   } else {
