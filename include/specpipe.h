@@ -226,9 +226,10 @@ int sp_stage_free_pages(const sp_stage* stage);
  * over 4-bit storage are those over the held values, with sums, softmax statistics and norms in float32.  An infinity
  * is held as +-6 * 2^125, a NaN as zero; what is read back is always finite.
  *
- * SP_FLAG_FP4_KV: d_head 64 or 128, any stage shape.  The slab holds d_head / 2 bytes of codes per (slot, head) row in
- * the layout above and, behind all code planes, four bytes of scales per row in planes of the same order; it is written
- * and read through sp_kv_store, sp_kv_load, sp_stage_append and sp_stage_forward (sp_sizes reports the code planes).
+ * SP_FLAG_FP4_KV: d_head 64 or 128, any stage shape, kv_slots up to SP_FP4_MAX_SLOTS (else SP_E_UNSUPPORTED).  The slab
+ * holds d_head / 2 bytes of codes per (slot, head) row in the layout above and, behind all code planes, four bytes of
+ * scales per row in planes of the same order; it is written and read through sp_kv_store, sp_kv_load, sp_stage_append and
+ * sp_stage_forward (sp_sizes reports the code planes).
  * Inserting, pruning, compaction and pages work as for the other caches.
  * SP_FLAG_FP4_WEIGHTS: the shapes SP_FLAG_PACKED_WEIGHTS takes, not together with it; the vocabulary matrix of the
  * output head stays bf16, row-major. */
@@ -236,6 +237,7 @@ int sp_stage_free_pages(const sp_stage* stage);
 /* Bytes of a packed [n_rows][n_cols] matrix; 0 if it cannot be packed: n_rows % 16 == 0, n_cols % 32 == 0, both up to
  * SP_FP4_MAX_DIM.  (Storage is in pieces of 16 rows x 256 columns: a last piece may be part empty.) */
 #define SP_FP4_MAX_DIM (1 << 17)
+#define SP_FP4_MAX_SLOTS ((1 << 25) - 1)
 size_t sp_fp4_matrix_bytes(int32_t n_rows, int32_t n_cols);
 
 /* Load-time conversion of a bf16 [n_rows][n_cols] matrix to 4 bits, and back to the bf16 values held.  Pointers are

@@ -98,6 +98,7 @@ int check_config(const sp_config* c) {
   if (!(c->rms_eps > 0.f) || !(c->rope_theta > 1.f)) return SP_E_INVALID;
   if ((c->flags & (SP_FLAG_FP4_KV | SP_FLAG_FP4_WEIGHTS)) && c->dtype != SP_BF16) return SP_E_UNSUPPORTED;
   if ((c->flags & SP_FLAG_FP4_WEIGHTS) && (c->flags & SP_FLAG_PACKED_WEIGHTS)) return SP_E_INVALID;
+  if ((c->flags & SP_FLAG_FP4_KV) && c->kv_slots > SP_FP4_MAX_SLOTS) return SP_E_UNSUPPORTED;
   if (c->flags & SP_FLAG_PAGED_KV) {
     // a page holds whole 32-slot attention tiles
     const int pg = c->page_slots;
@@ -720,6 +721,13 @@ static void plan_segments(const sp_stage* s, const FwdBatch& b, void* x_out, Att
   }
 }
 
+// The split of the attention's work, for the kernels that have one.  False: it does not fit the workspace or a grid.
+static bool split_work(const sp_stage* s, AttnPlan& plan) {
+  const sp_config& c = s->cfg;
+  if (s->geom.scales) return attn_split_fp4(plan, c.n_q_heads, c.n_kv_heads, s->n_cu, s->ws.attn_units) && plan.total_items <= 65535;
+  return !s->fast || attn_split(plan, c.n_q_heads, c.n_kv_heads, s->n_cu, s->ws.attn_units);
+}
+
 int sp_stage_forward(sp_stage* s, int32_t n_req, const int32_t* req_ids, const int32_t* first_node,
                      const int32_t* n_nodes, const void* x_in, void* x_out, sp_stream stream) {
   FwdBatch b;
@@ -739,7 +747,7 @@ int sp_stage_forward(sp_stage* s, int32_t n_req, const int32_t* req_ids, const i
   AttnPlan plan;
   plan_segments(s, b, x_out, plan);
   const bool kv4 = s->geom.scales != nullptr, normed = !s->norms.empty();
-  if ((s->fast || kv4) && !attn_split(plan, nq, nkv, s->n_cu, w.attn_units)) return SP_E_CAPACITY;
+  if (!split_work(s, plan)) return SP_E_CAPACITY;
 
   const size_t strideD = (size_t)M * d;
   // Complete projections, and in float32 the joined one, rotate a few columns of a head at a time: heads that are normed, or held
@@ -1025,7 +1033,7 @@ int sp_stage_attention(sp_stage* s, int32_t layer, int32_t n_req, const int32_t*
   AttnPlan plan;
   plan_segments(s, b, nullptr, plan);
   const bool kv4 = s->geom.scales != nullptr;
-  if ((s->fast || kv4) && !attn_split(plan, nq, nkv, s->n_cu, w.attn_units)) return SP_E_CAPACITY;
+  if (!split_work(s, plan)) return SP_E_CAPACITY;
   ProfScope p(s, SP_K_ATTENTION, st);
   hipError_t e;
   if (kv4) {

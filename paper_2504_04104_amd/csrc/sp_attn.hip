@@ -41,6 +41,22 @@ struct AttnArgs {
   const AttnPlan* plan;     // device copy of the call's plan (written by the kernel that opens the forward)
 };
 
+// Online softmax of a wave over QT tiles of 16 query rows.  mrun is the running maximum of the raw scores q.k; negm =
+// -mrun*sc (0 while mrun is -inf), so that exp2(fma(s, sc, negm)) is the softmax weight.
+template <int QT>
+struct AttnState {
+  f32x4_t o[QT][8];
+  float mrun[QT], lrun[QT], negm[QT];
+  __device__ __forceinline__ void init() {
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      mrun[t] = -INFINITY; lrun[t] = 0.f; negm[t] = 0.f;
+#pragma unroll
+      for (int d = 0; d < 8; ++d) o[t][d] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+    }
+  }
+};
+#define ATTN_SC (0.08838834764831845f * 1.4426950408889634f)   // 1/sqrt(128) * log2(e)
 
 // A tile's rows lie in LDS as they do in memory, 256 bytes each, but that the 16-byte units of a row are exchanged by the row's
 // number (unit u is at place u ^ unit_swap(row)): the direct-to-LDS loads leave no room for padding.  Sixteen rows' fragments
@@ -66,6 +82,59 @@ __device__ __forceinline__ void attn_scores(f32x4_t (&sacc)[QT][2], const u32x4_
                                                               *reinterpret_cast<const bf16x8_t*>(&qf[t][s]),
                                                               sacc[t][t2], 0, 0, 0);
     }
+}
+
+// Scores of the tile with first slot s0, of a run that ends at w1, to weights (bf16 pairs, in the order of sacc's slots).
+template <int QT>
+__device__ __forceinline__ void attn_softmax(AttnState<QT>& st, const f32x4_t (&sacc)[QT][2], uint32_t (&pb)[QT][4],
+                                             const unsigned long long (&anc)[QT][SP_W], int s0, int w1, int P, int span, int kg) {
+  const float sc = ATTN_SC;
+  const bool tail = s0 + 32 > P || s0 + 32 > w1;   // tile touches the tree region or the run's end
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    float sv[8];
+#pragma unroll
+    for (int t2 = 0; t2 < 2; ++t2)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sv[t2 * 4 + i] = sacc[t][t2][i];
+    if (tail) {
+      // bits [n0, n0+64) of the row's 256-bit ancestor mask, n0 = first tree index of the tile
+      const int n0 = s0 - P;
+      unsigned long long win = 0ull;
+#pragma unroll
+      for (int w = 0; w < SP_W; ++w) {
+        const int sh = w * 64 - n0;
+        if (sh > -64 && sh < 64) win |= sh >= 0 ? (anc[t][w] << sh) : (anc[t][w] >> (-sh));
+      }
+      const int lim = w1 - s0, pfx = P - s0, tl = span - s0;   // offsets below: in run / committed / live
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int off = (j >> 2) * 16 + kg * 4 + (j & 3);
+        const bool vis = (off < lim) & ((off < pfx) | ((off < tl) & (bool)((win >> off) & 1ull)));
+        sv[j] = vis ? sv[j] : -INFINITY;
+      }
+    }
+    float mx = fmaxf(fmaxf(fmaxf(sv[0], sv[1]), fmaxf(sv[2], sv[3])), fmaxf(fmaxf(sv[4], sv[5]), fmaxf(sv[6], sv[7])));
+    // The running maximum only has to bound the scores, so it is raised (and the
+    // accumulators rescaled) only when some lane of the wave sees a larger score.
+    if (__builtin_amdgcn_ballot_w64(mx > st.mrun[t])) {
+      mx = quad_rows_max(mx);
+      const float mnew = fmaxf(st.mrun[t], mx);
+      const float alpha = (mnew == -INFINITY) ? 1.f : __builtin_amdgcn_exp2f((st.mrun[t] - mnew) * sc);  // 0 from -inf
+      st.lrun[t] *= alpha;
+#pragma unroll
+      for (int d = 0; d < 8; ++d) st.o[t][d] *= alpha;
+      st.mrun[t] = mnew;
+      st.negm[t] = (mnew == -INFINITY) ? 0.f : -mnew * sc;
+    }
+    float pv[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) pv[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(sv[j], sc, st.negm[t]));
+    st.lrun[t] += ((pv[0] + pv[1]) + (pv[2] + pv[3])) + ((pv[4] + pv[5]) + (pv[6] + pv[7]));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) pb[t][j] = pack_bf16x2(pv[2 * j], pv[2 * j + 1]);
+  }
+
 }
 
 // O^T += V^T P^T; va: the lane's places for the transposing reads.  Sixteen lanes read four slots x 16 columns, lane 4c + x of
@@ -308,7 +377,7 @@ __global__ void __launch_bounds__(64 * AW) k_attn_bf16(AttnArgs a) {
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
     st.lrun[t] = quad_rows_sum(st.lrun[t]);
-    st.mrun[t] = st.mrun[t] * attn_scale<8>();              // to the log2 domain (-inf stays -inf)
+    st.mrun[t] = st.mrun[t] * ATTN_SC;              // to the log2 domain (-inf stays -inf)
     if (kg == 0) s_m[wave][t * 16 + l15] = st.mrun[t];
   }
   __syncthreads();                       // every wave is done with its tiles; maxima are posted

@@ -150,6 +150,12 @@ __device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t buf, char* ds
   __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (__attribute__((address_space(3))) void*)dst, 16, lane_offset, offset, 0, NT ? 2 : 0);
 #endif
 }
+// The same with four bytes per lane.
+__device__ __forceinline__ void load_dword_to_lds(__amdgpu_buffer_rsrc_t buf, char* dst, int lane_offset) {
+#ifdef __HIP_DEVICE_COMPILE__
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (__attribute__((address_space(3))) void*)dst, 4, lane_offset, 0, 0, 0);
+#endif
+}
 // Waits until at most n of the wave's vector memory accesses are outstanding.
 #define SP_WAIT_VMEM(n) __builtin_amdgcn_s_waitcnt(0x0f70 | ((n) & 15) | (((n) >> 4) << 14))
 // A barrier that waits for no memory access: what has to have arrived is waited for explicitly.  The compiler moves no

@@ -14,7 +14,8 @@
 // The scale as a float whose exponent field is the stored byte (a byte of zero: cleared storage, whose codes are zeros too).
 __device__ __forceinline__ float fp4_scale(uint32_t biased) { return __uint_as_float(biased << 23); }
 
-// Eight codes, lowest bits first, as a bf16 matrix operand.
+// Eight codes, lowest bits first, as a bf16 matrix operand.  (The conversion takes the exponent field of the scale and nothing
+// else of it.)
 __device__ __forceinline__ u32x4_t fp4_to_bf16x8(uint32_t codes, float scale) {
   return (u32x4_t){__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0)),
                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1)),

@@ -128,3 +128,27 @@ inline bool attn_split(AttnPlan& plan, int n_q, int n_kv, int n_cu, size_t room)
   if (plan.loads == ATTN_STREAM && plan.n_seg > 1 && !plan.any_split) plan.loads = ATTN_STREAM_REGS;
   return true;
 }
+
+// The same for a cache in 4 bits: blocks of 16 query rows, workgroups of eight waves.  A tile of 32 slots of every wave (a round)
+// is 0.65 us; cutting ranges costs the merge, a launch and the partial rows: as much as six rounds for a block of rows per head,
+// as eight for more.  Us a call of the 8B shape (32 query heads, 8 KV heads of 128), whole / in chunks (rounds saved): one row
+// behind 1600 and 2000 slots 9.9 / 10.8 (6) and 10.6 / 10.2 (7), 16 rows behind 2000 and 4000 11.2 / 11.8 (7) and 16.3 / 12.7
+// (14), 64 behind 4000 and 8000 16.7 / 17.1 (8) and 26.8 / 22.3 (16), four requests of one or two rows behind 2000-4000
+// 15.6 / 12.6 (13).  Nor do more chunks pay than fill the CUs: four instead of two of 64 rows behind 4000 slots 17.1 -> 19.0.
+inline bool attn_split_fp4(AttnPlan& plan, int n_q, int n_kv, int n_cu, size_t room) {
+  const int g = n_q / n_kv;
+  plan.qt = 1;
+  int longest = 0;
+  bool shared = false;
+  for (int i = 0; i < plan.n_seg; ++i) {
+    longest = plan.seg_P[i] + plan.seg_T[i] > longest ? plan.seg_P[i] + plan.seg_T[i] : longest;
+    shared = shared || plan.seg_rows[i] * g > 16;
+  }
+  int want = n_cu / (attn_blocks(plan, g, 16) * n_kv);
+  const int rounds = (longest + 255) / 256;
+  if (want > 1 && rounds - (rounds + want - 1) / want <= (shared ? 8 : 6)) want = 1;
+  size_t units = attn_cut(plan, g, n_q, want);
+  while (units > room && want > 1) { want = (want + 1) / 2; units = attn_cut(plan, g, n_q, want); }
+  plan.loads = ATTN_SHARED;
+  return units <= room;
+}
