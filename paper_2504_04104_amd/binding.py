@@ -110,8 +110,9 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
         "sp_kv_store": [vp, C.c_int32, C.c_int32, C.c_int32, C.c_int32, vp, vp, vp],
         "sp_kv_load": [vp, C.c_int32, C.c_int32, C.c_int32, C.c_int32, vp, vp, vp],
         "sp_stage_set_head_norms": [vp, C.POINTER(sp_head_norms)],
-        "sp_stage_append": [vp, C.c_int32, C.c_int32, i32p, i32p, i32p, vp, vp, vp],
-        "sp_stage_attention": [vp, C.c_int32, C.c_int32, i32p, i32p, i32p, vp, vp, vp],
+        # (host arrays as addresses: a pointer object for each costs these short calls 0.3 us)
+        "sp_stage_append": [vp, C.c_int32, C.c_int32, vp, vp, vp, vp, vp, vp],
+        "sp_stage_attention": [vp, C.c_int32, C.c_int32, vp, vp, vp, vp, vp, vp],
         "sp_request_init": [vp, C.c_int32, C.c_int64, C.c_int32, C.c_int32, vp],
         "sp_stage_verify_head": [vp, C.POINTER(sp_head_weights), C.c_int32, i32p, i32p, i32p, vp, vp, vp, vp],
         "sp_stage_verify_head_noalloc": [vp, C.POINTER(sp_head_weights), C.c_int32, i32p, i32p, i32p, vp, vp, vp, vp],
@@ -179,6 +180,19 @@ def _f32(a: Optional[Sequence[float]]):
         return buf, (C.c_float * len(buf)).from_buffer(buf)
     arr = np.ascontiguousarray(np.asarray(a, dtype=np.float32))
     return arr, arr.ctypes.data_as(C.POINTER(C.c_float))
+
+
+def _ids(a: Sequence[int]):
+    """Plain integers as an array that ctypes takes by its address (`_at`); what array() does not take is numpy's to cast or
+    refuse, as in _i32."""
+    try:
+        return array.array("i", a)
+    except (TypeError, OverflowError):
+        return array.array("i", np.ascontiguousarray(np.asarray(a, dtype=np.int32)).tobytes())
+
+
+def _at(a) -> int:
+    return a.buffer_info()[0]
 
 
 def _check(rc: int, what: str):
@@ -343,34 +357,39 @@ class Stage:
         _check(self.lib.sp_stage_set_head_norms(self.handle, arr), "sp_stage_set_head_norms")
         self.head_norms = norms                  # keeps the gains alive
 
-    def _rows_tensor(self, t, rows: int, cols: int):
-        assert t.is_cuda and t.is_contiguous() and t.dtype == self.tdtype and t.shape == (rows, cols)
-        return C.c_void_p(t.data_ptr())
+    def _rows_at(self, t, rows: int, cols: int) -> int:
+        assert t.is_cuda and t.dtype is self.tdtype and t.dim() == 2 and t.shape[0] == rows and t.shape[1] == cols and t.is_contiguous()
+        return t.data_ptr()
+
+    def _counted(self, req_ids, n_nodes) -> tuple:
+        r, n = _ids(req_ids), _ids(n_nodes)
+        assert len(r) == len(n)
+        return r, n, sum(n)
 
     def append(self, layer: int, req_ids: Sequence[int], first_node: Sequence[int], n_nodes: Sequence[int], qkv, q_out=None):
         """sp_stage_append: qkv [sum n_nodes, (n_q + 2 n_kv) * d_head] -> the rotated queries [sum n_nodes, n_q * d_head]."""
         s = self.shape
-        ra, rp = _i32(req_ids)
-        fa, fp = _i32(first_node)
-        na, np_ = _i32(n_nodes)
-        rows, dq = int(sum(na)), s.n_q_heads * s.d_head
+        r, n, rows = self._counted(req_ids, n_nodes)
+        f = _ids(first_node)
+        assert len(f) == len(r)
+        dq = s.n_q_heads * s.d_head
         if q_out is None:
-            q_out = self.torch.empty(rows, dq, dtype=self.tdtype, device=self.device)
-        _check(self.lib.sp_stage_append(self.handle, layer, len(ra), rp, fp, np_,
-                                        self._rows_tensor(qkv, rows, dq + 2 * s.n_kv_heads * s.d_head),
-                                        self._rows_tensor(q_out, rows, dq), self._stream()), "sp_stage_append")
+            q_out = self.torch.empty(max(rows, 0), dq, dtype=self.tdtype, device=self.device)
+        _check(self.lib.sp_stage_append(self.handle, layer, len(r), _at(r), _at(f), _at(n),
+                                        self._rows_at(qkv, rows, dq + 2 * s.n_kv_heads * s.d_head),
+                                        self._rows_at(q_out, rows, dq), self._stream()), "sp_stage_append")
         return q_out
 
     def attention(self, layer: int, req_ids: Sequence[int], first_node: Sequence[int], n_nodes: Sequence[int], q, out=None):
         """sp_stage_attention: q [sum n_nodes, n_q * d_head] -> the attention output of the same shape."""
-        ra, rp = _i32(req_ids)
-        fa, fp = _i32(first_node)
-        na, np_ = _i32(n_nodes)
-        rows, dq = int(sum(na)), self.shape.n_q_heads * self.shape.d_head
+        r, n, rows = self._counted(req_ids, n_nodes)
+        f = _ids(first_node)
+        assert len(f) == len(r)
+        dq = self.shape.n_q_heads * self.shape.d_head
         if out is None:
-            out = self.torch.empty(rows, dq, dtype=self.tdtype, device=self.device)
-        _check(self.lib.sp_stage_attention(self.handle, layer, len(ra), rp, fp, np_, self._rows_tensor(q, rows, dq),
-                                           self._rows_tensor(out, rows, dq), self._stream()), "sp_stage_attention")
+            out = self.torch.empty_like(q)
+        _check(self.lib.sp_stage_attention(self.handle, layer, len(r), _at(r), _at(f), _at(n), self._rows_at(q, rows, dq),
+                                           self._rows_at(out, rows, dq), self._stream()), "sp_stage_attention")
         return out
 
     def kv_store(self, req: int, layer: int, first_slot: int, k, v):
@@ -684,24 +703,35 @@ def fp4_pack_weights(shape, layers: List[Dict[str, "object"]]):
     return out
 
 
+_workspace_bytes: Dict[tuple, int] = {}          # of products, by their sizes and device
+
+
 def fp4_product(x, w: Fp4Matrix, gated: bool = False, out=None):
     """sp_fp4_product: x [m, k] bf16 times the held weights, [m, n]; gated: the first half of the matrix's rows are gates,
     the second the up rows, and the result is silu(gate) * up, [m, n_rows / 2].  The workspace is torch's."""
     import torch
     lib = load_library()
-    if gated and w.n_rows % 32:
-        raise SpError(-9, "a gated product of %d rows" % w.n_rows)
-    n = w.n_rows // 2 if gated else w.n_rows
-    assert x.is_cuda and x.is_contiguous() and x.dtype == torch.bfloat16 and x.dim() == 2 and x.shape[1] == w.n_cols
-    m = int(x.shape[0])
+    device = x.device
+    if device.index != torch._C._cuda_getDevice():
+        with torch.cuda.device(device):
+            return fp4_product(x, w, gated, out)
+    n, k, m = w.n_rows, w.n_cols, x.shape[0]
+    if gated:
+        if n % 32:
+            raise SpError(-9, "a gated product of %d rows" % n)
+        n //= 2
+    assert x.is_cuda and x.dtype is torch.bfloat16 and x.dim() == 2 and x.shape[1] == k and x.is_contiguous()
     if out is None:
-        out = torch.empty(m, n, dtype=torch.bfloat16, device=x.device)
-    assert out.is_cuda and out.is_contiguous() and out.dtype == torch.bfloat16 and out.shape == (m, n)
-    with torch.cuda.device(x.device):
-        size = lib.sp_fp4_product_workspace(m, n, w.n_cols, int(gated))
-        work = torch.empty(size, dtype=torch.uint8, device=x.device) if size else None
-        _check(lib.sp_fp4_product(x.data_ptr(), m, w.data.data_ptr(), n, w.n_cols, int(gated), out.data_ptr(),
-                                  work.data_ptr() if size else None, size, _raw_stream(x.device)), "sp_fp4_product")
+        out = torch.empty(m, n, dtype=torch.bfloat16, device=device)
+    else:
+        assert out.device == device and out.dtype is torch.bfloat16 and out.shape == (m, n) and out.is_contiguous()
+    key = (m, n, k, gated, device.index)
+    size = _workspace_bytes.get(key)
+    if size is None:
+        size = _workspace_bytes[key] = lib.sp_fp4_product_workspace(m, n, k, int(gated))
+    work = torch.empty(size, dtype=torch.uint8, device=device) if size else None
+    _check(lib.sp_fp4_product(x.data_ptr(), m, w.data.data_ptr(), n, k, 1 if gated else 0, out.data_ptr(), work.data_ptr() if size else None,
+                              size, torch._C._cuda_getCurrentRawStream(device.index)), "sp_fp4_product")
     return out
 
 

@@ -486,7 +486,7 @@ int sp_fp4_pack_weights(const sp_config* cfg, const sp_layer_weights* in, const 
 
 size_t sp_fp4_product_workspace(int32_t m, int32_t n, int32_t k, int32_t gated) {
   if (m < 1 || m > SP_FP4_MAX_DIM || (gated != 0 && gated != 1) || !fp4_shape((int64_t)n << gated, k) || n % 16) return 0;
-  return sp_fp4_product_floats(m, n << gated, k, gated != 0, current_cus()) * sizeof(float);
+  return sp_fp4_product_floats(m, n << gated, k, current_cus()) * sizeof(float);
 }
 
 int sp_fp4_product(const void* x, int32_t m, const void* w, int32_t n, int32_t k, int32_t gated, void* out, void* workspace,

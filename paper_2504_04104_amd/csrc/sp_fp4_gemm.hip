@@ -3,17 +3,19 @@
 //
 // Weights lie in units of 16 rows x 256 columns, 2176 bytes in a row of memory: twice 64 x 16 bytes of codes, lane l of a wave
 // taking row l % 16 and the 32 columns (l / 16) * 32 .. of either half -- one group, one scale -- and 64 x 2 bytes of scales.
-// The units of 16 rows follow each other over the columns.  Which column of X a product's operand holds is free as long as
-// both sides agree: the four steps over a half take columns kg * 32 + j * 8 .. + 7 in lane kg.
+// The units of 16 rows (a strip) follow each other over the columns.  Which column of X a product's operand holds is free as long
+// as both sides agree: the four steps over a half take columns kg * 32 + j * 8 .. + 7 in lane kg.  A conversion instruction makes
+// two codes and their scale two bf16 values.
 //
-// A workgroup of eight waves owns NS strips of 16 weight rows and MT tiles of 16 rows of X, its waves cut the columns among
-// them, and their sums are added through LDS.  A conversion instruction makes two codes and their scale two bf16 values.
+// Two kernels: up to 16 rows of short products the waves of a workgroup share strips and cut the columns among them; elsewhere
+// they have strips of their own and share rows of X through LDS.  What bounds them: up to some forty rows the weights' way from
+// memory (28672 x 4096, 62 MB: one row 11.0 us, 5.7 TB/s; 28672 wide twice, 8192 deep, 249 MB: 44.6 us); more rows the matrix
+// cores' feeding, 200 rows of the last 172 us, 1.09 PFLOP/s.
 #include "sp_launch.h"
 #include "sp_fp4.h"
 
 #define UNIT_K 256
 #define UNIT_BYTES 2176
-#define GW 8                 // waves per workgroup
 
 enum { OUT_PARTS, OUT_ROWS, OUT_GATED };
 
@@ -22,130 +24,258 @@ struct Fp4GemmArgs {
   const char* W;
   void* out;                 // OUT_PARTS: float32 [S][M][N]; OUT_ROWS: bf16 [M][N]; OUT_GATED: bf16 [M][N / 2]
   int M, N, K, units, S;
-  int groups, row_blocks;    // of strips (OUT_GATED: of pairs of strips); of 16 * MT rows
-  bool frag_out;             // OUT_GATED: the rows' order
+  int tiles, row_blocks;     // workgroups over the strips; over the rows
+  bool frag, frag_out;       // X in fragment order, rows of units * UNIT_K columns, or row-major; OUT_GATED: the result's order
 };
 
 __device__ __forceinline__ float silu(float x) { return x / (1.f + __expf(-x)); }
 
-// NS: strips of a workgroup; OUT_GATED: half of them gate rows, the others the up rows that belong to them.
-template <int MT, int NS, int OUT, bool XFRAG, bool NT>
-__global__ void __launch_bounds__(64 * GW) k_fp4_gemm(Fp4GemmArgs a) {
-  constexpr int PF = NS >= 4 ? 2 : 4;              // units in flight per strip and wave
-  __shared__ f32x4_t s_sum[GW][MT * NS][64];
+// Up to 16 rows: the waves of a workgroup share NS strips and cut the columns among them; their sums are added through LDS.
+// Rows and weights come from memory in fragment order or as they are, PF units ahead: loads return in order, so that rows that are
+// asked for later than weights wait for those.
+// OUT_GATED: a strip is eight gate rows and the eight up rows that belong to them, lanes 0-7 and 8-15 of sixteen.
+template <int NS, int OUT, bool XFRAG>
+__global__ void __launch_bounds__(NS <= 2 ? 512 : 256) k_fp4_few(Fp4GemmArgs a) {
+  constexpr int NW = NS <= 2 ? 8 : 4, PF = NS <= 2 ? 4 : 2;
+  __shared__ f32x4_t s_sum[NW][NS][64];
   auto uni = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
   const int wave = uni((int)threadIdx.x >> 6), lane = threadIdx.x & 63, l15 = lane & 15, kg = lane >> 4;
-  // the row blocks of a group of strips on one XCD, one after the other
-  const int id = blockIdx.x, xcd = id & 7, local = id >> 3;
-  const int rb = uni(local % a.row_blocks), sg = uni((local / a.row_blocks) * 8 + xcd);
-  const int slice = uni(sg / a.groups), group = sg - slice * a.groups;
-  if (slice >= a.S) return;
-  const int row0 = rb * 16 * MT, rows = min(a.M - row0, 16 * MT);
+  const int slice = uni((int)blockIdx.x / a.tiles), strip0 = uni(((int)blockIdx.x - slice * a.tiles) * NS);
   const int strips = a.N >> 4;
-  int strip[NS];
-#pragma unroll
-  for (int i = 0; i < NS; ++i)
-    strip[i] = OUT == OUT_GATED ? (i < NS / 2 ? group * (NS / 2) + i : (strips >> 1) + group * (NS / 2) + i - NS / 2) : group * NS + i;
-  auto there = [&](int i) { return OUT == OUT_GATED ? group * (NS / 2) + (i < NS / 2 ? i : i - NS / 2) < (strips >> 1) : strip[i] < strips; };
-  const int su0 = (int)((long long)slice * a.units / a.S), su1 = (int)((long long)(slice + 1) * a.units / a.S);
-  const int u0 = su0 + (su1 - su0) * wave / GW, u1 = su0 + (su1 - su0) * (wave + 1) / GW;
+  const int su0 = slice * a.units / a.S, su1 = (slice + 1) * a.units / a.S;
+  const int u0 = uni(su0 + (su1 - su0) * wave / NW), u1 = uni(su0 + (su1 - su0) * (wave + 1) / NW);
 
-  // buffers: loads past the run, past the strips and past the rows return zeros without a memory access (what is to be checked
-  // is in the lane's offset: a scalar one is not part of the check)
-  const int xrows = XFRAG ? (rows + 15) & ~15 : rows;
-  const auto xb = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(a.X) + (size_t)row0 * a.K, (short)0, uni(xrows * a.K * 2), 0x00020000);
-  const int x_lane = XFRAG ? kg * 1024 + l15 * 16 : l15 * a.K * 2 + kg * 64;
-  const int x_tile = 16 * a.K * 2;
-
-  u32x4_t wq[PF][NS][2];
+  // Buffers: loads past the run, past the strips and past the rows return zeros without a memory access.  What is to be checked
+  // is in the lane's offset: a scalar one is not part of the check.
+  const int xk = XFRAG ? a.units * UNIT_K : a.K;
+  const auto xb = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(a.X), (short)0, (XFRAG ? 16 : a.M) * xk * 2, 0x00020000);
+  const int x_lane = XFRAG ? kg * 1024 + l15 * 16 : l15 * xk * 2 + kg * 64;
+  const int half = OUT == OUT_GATED ? (strips >> 1) * a.units * UNIT_BYTES : 0;              // from the gate rows to the up rows
+  u32x4_t xf[PF][8], wq[PF][NS][2];
   uint32_t wsc[PF][NS];
   auto fetch = [&](int p, int u) {
+    const bool run = u < u1;
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
-      const bool on = u < u1 && there(i);
-      const auto wb = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(a.W) + ((size_t)(on ? strip[i] : 0) * a.units + (on ? u : 0)) * UNIT_BYTES,
-                                                        (short)0, on ? UNIT_BYTES : 0, 0x00020000);
+      const int strip = strip0 + i;
+      const bool on = run && strip < strips;
+      const int unit_strip = OUT == OUT_GATED ? strip >> 1 : strip;
+      const auto wb = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(a.W) + ((size_t)(on ? unit_strip : 0) * a.units + (on ? u : 0)) * UNIT_BYTES,
+                                                        (short)0, on ? half + UNIT_BYTES : 0, 0x00020000);
+      int at = lane, up = 0;
+      if (OUT == OUT_GATED) { at = kg * 16 + (strip & 1) * 8 + (l15 & 7); up = l15 < 8 ? 0 : half; }
 #pragma unroll
-      for (int b = 0; b < 2; ++b) wq[p][i][b] = __builtin_amdgcn_raw_buffer_load_b128(wb, lane * 16, b * 1024, NT ? 2 : 0);
-      wsc[p][i] = __builtin_amdgcn_raw_buffer_load_b16(wb, lane * 2, 2048, NT ? 2 : 0);
+      for (int b = 0; b < 2; ++b) wq[p][i][b] = __builtin_amdgcn_raw_buffer_load_b128(wb, up + at * 16 + b * 1024, 0, 2);
+      wsc[p][i] = __builtin_amdgcn_raw_buffer_load_b16(wb, up + at * 2 + 2048, 0, 2);
+    }
+#pragma unroll
+    for (int step = 0; step < 8; ++step) {
+      const int k0 = (run ? u : 0) * UNIT_K + (step >> 2) * 128;
+      const int at = XFRAG ? (k0 >> 5) * 1024 + (step & 3) * 256 : k0 * 2 + (step & 3) * 16;
+      // (row-major: columns past the end meet weights of zero, but what lies behind a row may be anything)
+      const int off = run && (XFRAG || k0 + kg * 32 < a.K) ? x_lane : 0x7fffff00;
+      xf[p][step] = __builtin_amdgcn_raw_buffer_load_b128(xb, off, at, 0);
     }
   };
 #pragma unroll
   for (int p = 0; p < PF; ++p) fetch(p, u0 + p);
+  f32x4_t acc[NS];
+#pragma unroll
+  for (int i = 0; i < NS; ++i) acc[i] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+  for (int ub = u0; ub < u1; ub += PF) {
+#pragma unroll
+    for (int p = 0; p < PF; ++p) {
+      if (ub + p < u1) {
+#pragma unroll
+        for (int step = 0; step < 8; ++step) {
+#pragma unroll
+          for (int i = 0; i < NS; ++i) {
+            const u32x4_t wf = fp4_to_bf16x8(wq[p][i][step >> 2][step & 3], fp4_scale((wsc[p][i] >> (8 * (step >> 2))) & 255u));
+            acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, wf), __builtin_bit_cast(bf16x8_t, xf[p][step]),
+                                                             acc[i], 0, 0, 0);
+          }
+        }
+        fetch(p, ub + p + PF);
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < NS; ++i) s_sum[wave][i][lane] = acc[i];
+  __syncthreads();
+  // a lane's four sums: row l15 of X, rows kg * 4 .. + 3 of the strip
+  auto total = [&](int i, int ln) {
+    f32x4_t v = s_sum[0][i][ln];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) v += s_sum[w][i][ln];
+    return v;
+  };
+  const int strip = strip0 + wave;
+  if (wave >= NS || strip >= strips || l15 >= a.M || (OUT == OUT_GATED && lane >= 32)) return;
+  const f32x4_t v = total(wave, lane);
+  if constexpr (OUT == OUT_GATED) {
+    const f32x4_t up = total(wave, lane + 32);
+    *reinterpret_cast<uint2*>(reinterpret_cast<bf16_t*>(a.out) + row_at(a.frag_out, l15, strip * 8 + kg * 4, a.N >> 1)) =
+        uint2{pack_bf16x2(silu(v[0]) * up[0], silu(v[1]) * up[1]), pack_bf16x2(silu(v[2]) * up[2], silu(v[3]) * up[3])};
+  } else if constexpr (OUT == OUT_PARTS) {
+    *reinterpret_cast<f32x4_t*>(reinterpret_cast<float*>(a.out) + ((size_t)slice * a.M + l15) * a.N + strip * 16 + kg * 4) = v;
+  } else {
+    *reinterpret_cast<uint2*>(reinterpret_cast<bf16_t*>(a.out) + (size_t)l15 * a.N + strip * 16 + kg * 4) =
+        uint2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+  }
+}
 
+// The waves share the rows of X through LDS, which a load brings there without registers, and have NS strips each over all columns
+// of the slice.  A chunk is 128 columns, half a unit; loads are three chunks ahead, a chunk's rows before its weights, and go out
+// between the products: all at once behind the barrier they held up the matrix cores (4096 x 14336, 64 rows, four tiles and four
+// strips whole 91.8 us, 83.3 between).
+#define CHUNKS_AHEAD 3
+#define PANELS 4
+template <int MT, int NS, int OUT>
+__global__ void __launch_bounds__(256, MT * NS <= 16 ? 2 : 1) k_fp4_many(Fp4GemmArgs a) {
+  constexpr int PANEL = MT * 4096;
+  // arrays of their own, so that the compiler knows which loads a read has to wait for
+  __shared__ __attribute__((aligned(16))) char p0[PANEL];
+  __shared__ __attribute__((aligned(16))) char p1[PANEL];
+  __shared__ __attribute__((aligned(16))) char p2[PANEL];
+  __shared__ __attribute__((aligned(16))) char p3[PANEL];
+#define SP_PAN(i) ((i) == 0 ? p0 : (i) == 1 ? p1 : (i) == 2 ? p2 : p3)
+  auto uni = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+  const int wave = uni((int)threadIdx.x >> 6), lane = threadIdx.x & 63, l15 = lane & 15, kg = lane >> 4;
+  // the row blocks of a column tile on one XCD, one after the other
+  const int id = blockIdx.x, local = id >> 3;
+  const int rb = uni(local % a.row_blocks), ts = uni((local / a.row_blocks) * 8 + (id & 7));
+  const int slice = uni(ts / a.tiles), tile = uni(ts - slice * a.tiles);
+  if (slice >= a.S) return;
+  const int c_begin = uni((int)((long long)slice * a.units / a.S) * 2), c_end = uni(min((int)((long long)(slice + 1) * a.units / a.S) * 2, (a.K + 127) / 128));
+  const int strips = a.N >> 4, t0 = rb * MT;
+  // gated: the first half of the wave's strips are gate rows, the second the up rows of the same columns
+  const int own = OUT == OUT_GATED ? NS / 2 : NS, strip0 = (tile * 4 + wave) * own;
+  const int strip_bytes = a.units * UNIT_BYTES;
+  const char* w[NS];
+  int live[NS];              // bytes
+#pragma unroll
+  for (int i = 0; i < NS; ++i) {
+    const int strip = strip0 + i % own + i / own * (strips >> 1);
+    live[i] = strip0 + i % own < (OUT == OUT_GATED ? strips >> 1 : strips) ? strip_bytes : 0;
+    w[i] = a.W + (live[i] ? (size_t)strip * strip_bytes : 0);
+  }
+  // A load to LDS brings a tile's 16 rows x 32 columns, lane (l15, kg) 16 bytes of row l15: a kilobyte of X in fragment order, or
+  // 64 bytes of each row where they lie one after the other.  Rows past the last are past the buffer's end.
+  const int xk = a.frag ? a.units * UNIT_K : a.K, k_step = a.frag ? 1024 : 64, lane16 = lane * 16;
+  const int x_rows = min(a.M - t0 * 16, MT * 16), x_bytes = (a.frag ? (x_rows + 15) & ~15 : x_rows) * xk * 2, x_blocks = min(xk >> 5, c_end * 4);
+  const bf16_t* xblk = a.X + (size_t)t0 * 16 * xk;
+  const int x_lane = a.frag ? lane16 : l15 * xk * 2 + kg * 16;
+
+  // the word with the lane's two scales, and the turn that brings the first into the exponent field
+  const int scale_at = 2048 + (lane & 62) * 2, turn = (lane & 1) * 16 + 9;
+  u32x4_t wb[PANELS][NS];
+  uint32_t ws[PANELS][NS];
   f32x4_t acc[MT][NS];
 #pragma unroll
   for (int t = 0; t < MT; ++t)
 #pragma unroll
     for (int i = 0; i < NS; ++i) acc[t][i] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-
-  for (int ub = u0; ub < u1; ub += PF) {
-#pragma unroll
-    for (int p = 0; p < PF; ++p) {
-      const int u = ub + p;
-      if (u < u1) {
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          u32x4_t xf[MT][4];
-          const int k0 = u * UNIT_K + b * 128;
-#pragma unroll
-          for (int t = 0; t < MT; ++t)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              // (columns past the end meet weights of zero; what lies behind a row may be anything)
-              int off = x_lane + t * x_tile + (XFRAG ? (k0 >> 5) * 1024 : k0 * 2);
-              if (!XFRAG) off = k0 + kg * 32 < a.K ? off : 0x7fffff00;
-              xf[t][j] = __builtin_amdgcn_raw_buffer_load_b128(xb, off + j * (XFRAG ? 256 : 16), 0, 0);
-            }
-#pragma unroll
-          for (int i = 0; i < NS; ++i) {
-            const float sc = fp4_scale((wsc[p][i] >> (8 * b)) & 255u);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const u32x4_t wf = fp4_to_bf16x8(wq[p][i][b][j], sc);
-#pragma unroll
-              for (int t = 0; t < MT; ++t)
-                acc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, wf), __builtin_bit_cast(bf16x8_t, xf[t][j]),
-                                                                    acc[t][i], 0, 0, 0);
-            }
-          }
-        }
-        fetch(p, u + PF);
-      }
-    }
+#define SP_LOAD_X(I, C)                                                                                                \
+  {                                                                                                                    \
+    const int k_ = (C) * 4 + wave;                                                                                     \
+    const auto xb_ = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(xblk), (short)0, k_ < x_blocks ? x_bytes : 0, 0x00020000); \
+    _Pragma("unroll") for (int t = 0; t < MT; ++t)                                                                     \
+        load_to_lds(xb_, SP_PAN(I) + (t * 4 + wave) * 1024, x_lane + t * 32 * xk, k_ * k_step);                        \
   }
+#define SP_LOAD_W(I, C, s)                                                                                             \
+  {                                                                                                                    \
+    const auto wr_ = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(w[s]), (short)0, (C) < c_end ? live[s] : 0, 0x00020000); \
+    wb[I][s] = __builtin_amdgcn_raw_buffer_load_b128(wr_, lane16 + ((I) & 1) * 1024, ((C) >> 1) * UNIT_BYTES, 0);      \
+    ws[I][s] = __builtin_amdgcn_raw_buffer_load_b32(wr_, scale_at, ((C) >> 1) * UNIT_BYTES, 0);                        \
+  }
+#define SP_READ(I, j, Q)                                                                                               \
+  _Pragma("unroll") for (int t = 0; t < MT; ++t)                                                                       \
+      xq[Q][t] = *reinterpret_cast<const u32x4_t*>(SP_PAN(I) + t * 4096 + kg * 1024 + (j) * 256 + l15 * 16);
+  // A quarter of a chunk's products, between them the reads for the next quarter and a part of the loads
+#define SP_STEP(I, j, LOADS)                                                                                           \
+  {                                                                                                                    \
+    if ((j) < 3) { SP_READ(I, (j) + 1, ((j) + 1) & 1) } else { SP_READ(((I) + 1) % PANELS, 0, 0) }                     \
+    LOADS                                                                                                              \
+    _Pragma("unroll") for (int i = 0; i < NS; ++i) {                                                                   \
+      const u32x4_t wf = fp4_to_bf16x8(wb[I][i][j], __uint_as_float(__builtin_amdgcn_alignbit(ws[I][i], ws[I][i], turn + ((I) & 1) * 8))); \
+      _Pragma("unroll") for (int t = 0; t < MT; ++t)                                                                   \
+          acc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, wf),                        \
+                                                              __builtin_bit_cast(bf16x8_t, xq[(j) & 1][t]), acc[t][i], 0, 0, 0); \
+    }                                                                                                                  \
+    __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);                                                                 \
+    _Pragma("unroll") for (int n = 0; n < MT * NS; ++n) {                                                              \
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                                                               \
+      __builtin_amdgcn_sched_group_barrier(0x002, MT <= 4 ? 2 : 1, 0);                                                 \
+      if (n % NS == 0) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);                                              \
+      if (n % NS == 1) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);                                              \
+    }                                                                                                                  \
+    __builtin_amdgcn_sched_barrier(0);                                                                                 \
+  }
+#define SP_CHUNK(I, C)                                                                                                 \
+  {                                                                                                                    \
+    SP_WAIT_VMEM(MT + 2 * 2 * NS);                                                                                     \
+    bare_barrier();                                                                                                    \
+    const int ahead_ = (C) + CHUNKS_AHEAD;                                                                             \
+    SP_STEP(I, 0, SP_LOAD_X(((I) + CHUNKS_AHEAD) % PANELS, ahead_))                                                    \
+    SP_STEP(I, 1, _Pragma("unroll") for (int s = 0; s < NS; s += 2) SP_LOAD_W(((I) + CHUNKS_AHEAD) % PANELS, ahead_, s)) \
+    SP_STEP(I, 2, _Pragma("unroll") for (int s = 1; s < NS; s += 2) SP_LOAD_W(((I) + CHUNKS_AHEAD) % PANELS, ahead_, s)) \
+    SP_STEP(I, 3, )                                                                                                    \
+  }
+#define SP_CHUNK_PRODUCTS(I) { SP_STEP(I, 0, ) SP_STEP(I, 1, ) SP_STEP(I, 2, ) SP_STEP(I, 3, ) }
+#pragma unroll
+  for (int p = 0; p < CHUNKS_AHEAD; ++p) {
+    SP_LOAD_X(p, c_begin + p)
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int s = 0; s < NS; ++s) SP_LOAD_W(p, c_begin + p, s)
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  SP_WAIT_VMEM(2 * (MT + 2 * NS) + 2 * NS);
+  bare_barrier();
+  u32x4_t xq[2][MT];
+  SP_READ(0, 0, 0)
+  int c = c_begin;
+  for (; c + 4 <= c_end; c += 4) {
+    SP_CHUNK(0, c)
+    SP_CHUNK(1, c + 1)
+    SP_CHUNK(2, c + 2)
+    SP_CHUNK(3, c + 3)
+  }
+  SP_WAIT_VMEM(0);
+  if (c < c_end) {                                  // up to three are left, and have been asked for
+    bare_barrier();
+    SP_CHUNK_PRODUCTS(0)
+    if (c + 1 < c_end) SP_CHUNK_PRODUCTS(1)
+    if (c + 2 < c_end) SP_CHUNK_PRODUCTS(2)
+  }
+#undef SP_CHUNK_PRODUCTS
+#undef SP_STEP
+#undef SP_LOAD_X
+#undef SP_LOAD_W
+#undef SP_CHUNK
+#undef SP_READ
+#undef SP_PAN
 
+  // a lane's four sums: row t * 16 + l15 of X, rows kg * 4 .. + 3 of the strip
 #pragma unroll
-  for (int t = 0; t < MT; ++t)
+  for (int t = 0; t < MT; ++t) {
+    const int m = (t0 + t) * 16 + l15;
+    if (m >= a.M) continue;
 #pragma unroll
-    for (int i = 0; i < NS; ++i) s_sum[wave][t * NS + i][lane] = acc[t][i];
-  __syncthreads();
-  // a lane's four sums: row t * 16 + l15 of X, weight rows kg * 4 .. + 3 of the strip
-  auto total = [&](int f) {
-    f32x4_t v = s_sum[0][f][lane];
-#pragma unroll
-    for (int w = 1; w < GW; ++w) v += s_sum[w][f][lane];
-    return v;
-  };
-  if constexpr (OUT == OUT_GATED) {
-    for (int f = wave; f < MT * (NS / 2); f += GW) {
-      const int t = f / (NS / 2), i = f - t * (NS / 2), m = t * 16 + l15;
-      const f32x4_t gt = total(t * NS + i), up = total(t * NS + NS / 2 + i);
-      if (m >= rows || !there(i)) continue;
-      const int n = strip[0] * 16 + i * 16 + kg * 4;
-      *reinterpret_cast<uint2*>(reinterpret_cast<bf16_t*>(a.out) + row_at(a.frag_out, row0 + m, n, a.N >> 1)) =
-          uint2{pack_bf16x2(silu(gt[0]) * up[0], silu(gt[1]) * up[1]), pack_bf16x2(silu(gt[2]) * up[2], silu(gt[3]) * up[3])};
-    }
-  } else {
-    for (int f = wave; f < MT * NS; f += GW) {
-      const int t = f / NS, i = f - t * NS, m = t * 16 + l15;
-      const f32x4_t v = total(f);
-      if (m >= rows || !there(i)) continue;
-      const int n = strip[0] * 16 + i * 16 + kg * 4;
-      if constexpr (OUT == OUT_PARTS)
-        *reinterpret_cast<f32x4_t*>(reinterpret_cast<float*>(a.out) + ((size_t)slice * a.M + row0 + m) * a.N + n) = v;
-      else
-        *reinterpret_cast<uint2*>(reinterpret_cast<bf16_t*>(a.out) + (size_t)(row0 + m) * a.N + n) = uint2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+    for (int i = 0; i < own; ++i) {
+      if (!live[i]) continue;
+      const f32x4_t v = acc[t][i];
+      const int col = (strip0 + i) * 16 + kg * 4;
+      if constexpr (OUT == OUT_GATED) {
+        const f32x4_t up = acc[t][i + NS / 2];
+        *reinterpret_cast<uint2*>(reinterpret_cast<bf16_t*>(a.out) + row_at(a.frag_out, m, col, a.N >> 1)) =
+            uint2{pack_bf16x2(silu(v[0]) * up[0], silu(v[1]) * up[1]), pack_bf16x2(silu(v[2]) * up[2], silu(v[3]) * up[3])};
+      } else if constexpr (OUT == OUT_PARTS) {
+        *reinterpret_cast<f32x4_t*>(reinterpret_cast<float*>(a.out) + ((size_t)slice * a.M + m) * a.N + col) = v;
+      } else {
+        *reinterpret_cast<uint2*>(reinterpret_cast<bf16_t*>(a.out) + (size_t)m * a.N + col) =
+            uint2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+      }
     }
   }
 }
@@ -232,76 +362,101 @@ hipError_t sp_launch_fp4_unpack(const void* in, void* out, int N, int K, hipStre
   return hipGetLastError();
 }
 
-// How a product is cut: tiles of rows and strips of a workgroup, and slices of the columns where the strips leave CUs idle.
+// How a product is cut: tiles of rows (0: the kernel for few rows) and strips of a workgroup, and slices of the columns, whose
+// sums are joined by a launch of their own (`join` us; 0 where whoever takes the partial sums adds them up).  What is least by
+// these times, which are those of a chunk of 128 columns with one workgroup on a CU, in 112 chunks: 0.21 us for one tile and two
+// strips, 0.27 for two tiles, 0.46 and 0.70 for four with two and four strips, 0.93 for five, 1.22 for seven; a unit of a wave of
+// the kernel for few rows 1 us and more with every row; a megabyte of partial sums 0.3.  Workgroups past the CUs take turns: two
+// at a time on a CU are not faster than one after the other.  Us a call as chosen, and next to it: 64 rows, 28672 x 4096 gated,
+// tiles x strips 4 x 2 20.3 (2 x 2 22.1, 4 x 4 26.8), 100 rows 4 x 4 27.3 (4 x 2 37.0), 160 rows 5 x 4 35.1 (4 x 4 46.8), 200 rows
+// 7 x 4 44.2 (4 x 4 48.5), 256 rows 4 x 4 50.6 (7 x 4 85.1); 4096 x 14336, 17 rows 2 x 2 in 8 slices 12.4 (in 4 13.9, whole 33.3),
+// 64 rows in 4 14.8 (in 8 16.8), 200 rows 4 x 4 in 4 30.9 (2 x 2 whole 35.0); one row, 4096 x 4096 with the kernel for few rows 6.8
+// (one tile in 4 slices 9.7), 4096 x 14336 with one tile in 8 slices 10.8 (few rows' 11.4), 28672 x 4096 gated 11.0 (few rows' 15.7).
 struct Fp4Split { int mt, ns, S; };
-static Fp4Split split_of(int M, int N, int K, bool gated, int n_cu) {
-  Fp4Split f;
+static Fp4Split split_of(int M, int N, int K, int n_cu, float join, int most_slices) {
+  static const struct { int mt, ns; float us; } tiled[] = {{1, 2, .21f}, {2, 2, .27f}, {4, 2, .46f}, {4, 4, .70f}, {5, 4, .93f}, {7, 4, 1.22f}};
+  static const struct { int ns, waves; float us, us_row; } few[] = {{1, 8, 1.f, .07f}, {2, 8, 1.6f, .06f}, {4, 4, 1.f, .06f}};
   const int units = (K + UNIT_K - 1) / UNIT_K, strips = N / 16;
-  f.mt = M <= 16 ? 1 : M <= 32 ? 2 : 4;
-  const int blocks = (M + 16 * f.mt - 1) / (16 * f.mt);
-  f.ns = strips * blocks >= 4 * n_cu ? 4 : strips * blocks >= 2 * n_cu || gated ? 2 : 1;
-  const int wgs = (strips + f.ns - 1) / f.ns * blocks;
-  f.S = n_cu / wgs;
-  if (f.S > units / GW) f.S = units / GW;
-  if (f.S < 1) f.S = 1;
-  return f;
+  Fp4Split best = {0, 1, 1};
+  float least = 1e30f;
+  if (M <= 16 && sp_fp4_bytes(N, K) < 1u << 31)     // (few rows: gate and up rows in one buffer)
+    for (const auto& f : few) {
+      const float us = (float)(((strips + f.ns - 1) / f.ns + n_cu - 1) / n_cu) * ((units + f.waves - 1) / f.waves) * (f.us + f.us_row * M);
+      if (us < least) { least = us; best = {0, f.ns, 1}; }
+    }
+  for (const auto& t : tiled) {
+    const long long wgs = (long long)((strips + 4 * t.ns - 1) / (4 * t.ns)) * ((M + 16 * t.mt - 1) / (16 * t.mt));
+    for (int S = 1; S <= most_slices && S <= units; ++S) {
+      if (S > 1 && wgs * S > 2 * n_cu) break;
+      const float us = (float)((wgs * S + n_cu - 1) / n_cu) * ((units + S - 1) / S * 2) * t.us + (S > 1 ? join + (float)S * M * N * 1.2e-6f : 0.f);
+      if (us < least) { least = us; best = {t.mt, t.ns, S}; }
+    }
+  }
+  return best;
 }
-size_t sp_fp4_product_floats(int M, int N, int K, bool gated, int n_cu) {
-  const Fp4Split f = split_of(M, N, K, gated, n_cu);
+#define JOIN_US 3.5f
+#define MOST_SLICES 16
+size_t sp_fp4_product_floats(int M, int N, int K, int n_cu) {
+  const Fp4Split f = split_of(M, N, K, n_cu, JOIN_US, MOST_SLICES);
   return f.S > 1 ? (size_t)f.S * M * N : 0;
 }
 
-template <int MT, int NS, int OUT, bool XFRAG>
-static void go(const Fp4GemmArgs& a, hipStream_t st) {
-  const int sgs = (a.groups * a.S + 7) / 8 * 8;
-  const dim3 grid(sgs * a.row_blocks), block(64 * GW);
-  if (a.row_blocks == 1) hipLaunchKernelGGL((k_fp4_gemm<MT, NS, OUT, XFRAG, true>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((k_fp4_gemm<MT, NS, OUT, XFRAG, false>), grid, block, 0, st, a);
+template <int NS, int OUT>
+static void go_few(Fp4GemmArgs& a, hipStream_t st) {
+  a.tiles = (a.N / 16 + NS - 1) / NS;
+  const dim3 grid(a.tiles * a.S), block(NS <= 2 ? 512 : 256);
+  if (a.frag) hipLaunchKernelGGL((k_fp4_few<NS, OUT, true>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((k_fp4_few<NS, OUT, false>), grid, block, 0, st, a);
 }
-template <int OUT, bool XFRAG>
+template <int MT, int NS, int OUT>
+static void go_many(Fp4GemmArgs& a, hipStream_t st) {
+  const int strips = OUT == OUT_GATED ? a.N / 32 : a.N / 16, per = OUT == OUT_GATED ? 2 * NS : 4 * NS;
+  a.row_blocks = (a.M + 16 * MT - 1) / (16 * MT);
+  a.tiles = (strips + per - 1) / per;
+  hipLaunchKernelGGL((k_fp4_many<MT, NS, OUT>), dim3((a.tiles * a.S + 7) / 8 * 8 * a.row_blocks), dim3(256), 0, st, a);
+}
+template <int OUT>
 static hipError_t launch(const Fp4Split& f, Fp4GemmArgs& a, hipStream_t st) {
-  const int per = OUT == OUT_GATED ? f.ns / 2 : f.ns, have = OUT == OUT_GATED ? a.N / 32 : a.N / 16;
-  a.groups = (have + per - 1) / per;
-  a.row_blocks = (a.M + 16 * f.mt - 1) / (16 * f.mt);
-#define SP_FP4_MT(NSV)                                                                          \
-  switch (f.mt) {                                                                               \
-    case 1: go<1, NSV, OUT, XFRAG>(a, st); break;                                               \
-    case 2: go<2, NSV, OUT, XFRAG>(a, st); break;                                               \
-    default: go<4, NSV, OUT, XFRAG>(a, st); break;                                              \
+  switch (f.mt * 8 + f.ns) {
+    case 1: go_few<1, OUT>(a, st); break;
+    case 2: go_few<2, OUT>(a, st); break;
+    case 4: go_few<4, OUT>(a, st); break;
+    case 1 * 8 + 2: go_many<1, 2, OUT>(a, st); break;
+    case 2 * 8 + 2: go_many<2, 2, OUT>(a, st); break;
+    case 4 * 8 + 2: go_many<4, 2, OUT>(a, st); break;
+    case 4 * 8 + 4: go_many<4, 4, OUT>(a, st); break;
+    case 5 * 8 + 4: go_many<5, 4, OUT>(a, st); break;
+    case 7 * 8 + 4: go_many<7, 4, OUT>(a, st); break;
+    default: return hipErrorInvalidValue;
   }
-  if (f.ns == 4) SP_FP4_MT(4)
-  else if (f.ns == 2) SP_FP4_MT(2)
-  else if constexpr (OUT != OUT_GATED) SP_FP4_MT(1)
-#undef SP_FP4_MT
   return hipGetLastError();
 }
 
 hipError_t sp_launch_fp4_parts(const bf16_t* X, bool frag, const void* W, float* out, int M, int N, int K, int n_cu, size_t part_floats,
                                int* S_out, hipStream_t st) {
-  Fp4Split f = split_of(M, N, K, false, n_cu);
+  Fp4Split f = split_of(M, N, K, n_cu, 0.f, MOST_SLICES);
   while (f.S > 1 && (size_t)f.S * M * N > part_floats) --f.S;
   if ((size_t)f.S * M * N > part_floats) return hipErrorInvalidValue;
   *S_out = f.S;
-  Fp4GemmArgs a{X, (const char*)W, out, M, N, K, (K + UNIT_K - 1) / UNIT_K, f.S, 0, 0, false};
-  return frag ? launch<OUT_PARTS, true>(f, a, st) : launch<OUT_PARTS, false>(f, a, st);
+  Fp4GemmArgs a{X, (const char*)W, out, M, N, K, (K + UNIT_K - 1) / UNIT_K, f.S, 0, 0, frag, false};
+  return launch<OUT_PARTS>(f, a, st);
 }
 hipError_t sp_launch_fp4_gateup(const bf16_t* X, bool frag, const void* W, bf16_t* act, int M, int F, int K, int n_cu, hipStream_t st) {
-  Fp4Split f = split_of(M, 2 * F, K, true, n_cu);
-  f.S = 1;
-  Fp4GemmArgs a{X, (const char*)W, act, M, 2 * F, K, (K + UNIT_K - 1) / UNIT_K, 1, 0, 0, frag};
-  return frag ? launch<OUT_GATED, true>(f, a, st) : launch<OUT_GATED, false>(f, a, st);
+  const Fp4Split f = split_of(M, 2 * F, K, n_cu, 0.f, 1);
+  Fp4GemmArgs a{X, (const char*)W, act, M, 2 * F, K, (K + UNIT_K - 1) / UNIT_K, 1, 0, 0, frag, frag};
+  return launch<OUT_GATED>(f, a, st);
 }
-hipError_t sp_launch_fp4_product(const bf16_t* X, const void* W, bool gated, bf16_t* out, float* part, int M, int N, int K, int n_cu,
+hipError_t sp_launch_fp4_product(const bf16_t* X, const void* W, bool gated, bf16_t* out, float* work, int M, int N, int K, int n_cu,
                                  hipStream_t st) {
-  Fp4Split f = split_of(M, N, K, gated, n_cu);
-  Fp4GemmArgs a{X, (const char*)W, out, M, N, K, (K + UNIT_K - 1) / UNIT_K, f.S, 0, 0, false};
-  if (f.S == 1) return gated ? launch<OUT_GATED, false>(f, a, st) : launch<OUT_ROWS, false>(f, a, st);
-  a.out = part;
-  hipError_t e = launch<OUT_PARTS, false>(f, a, st);
+  const Fp4Split f = split_of(M, N, K, n_cu, JOIN_US, MOST_SLICES);
+  Fp4GemmArgs a{X, (const char*)W, out, M, N, K, (K + UNIT_K - 1) / UNIT_K, f.S, 0, 0, false, false};
+  if (f.S == 1) return gated ? launch<OUT_GATED>(f, a, st) : launch<OUT_ROWS>(f, a, st);
+  a.out = work;
+  const hipError_t e = launch<OUT_PARTS>(f, a, st);
   if (e != hipSuccess) return e;
   const size_t four = (size_t)M * (gated ? N / 2 : N) / 4;
   const dim3 grid((unsigned)((four + 255) / 256 < 4096 ? (four + 255) / 256 : 4096));
-  if (gated) hipLaunchKernelGGL(k_fp4_fold<true>, grid, dim3(256), 0, st, part, out, f.S, M, N);
-  else hipLaunchKernelGGL(k_fp4_fold<false>, grid, dim3(256), 0, st, part, out, f.S, M, N);
+  if (gated) hipLaunchKernelGGL(k_fp4_fold<true>, grid, dim3(256), 0, st, work, out, f.S, M, N);
+  else hipLaunchKernelGGL(k_fp4_fold<false>, grid, dim3(256), 0, st, work, out, f.S, M, N);
   return hipGetLastError();
 }

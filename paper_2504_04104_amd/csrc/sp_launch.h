@@ -196,7 +196,7 @@ hipError_t sp_launch_fp4_parts(const bf16_t* X, bool frag, const void* W, float*
                                int* S_out, hipStream_t st);
 hipError_t sp_launch_fp4_gateup(const bf16_t* X, bool frag, const void* W, bf16_t* act, int M, int F, int K, int n_cu, hipStream_t st);
 // out: bf16 [M][N], or gated [M][N / 2]; part: as many floats as sp_fp4_product_floats says
-size_t sp_fp4_product_floats(int M, int N, int K, bool gated, int n_cu);
+size_t sp_fp4_product_floats(int M, int N, int K, int n_cu);
 hipError_t sp_launch_fp4_product(const bf16_t* X, const void* W, bool gated, bf16_t* out, float* part, int M, int N, int K, int n_cu,
                                  hipStream_t st);
 // row descriptors of a call's rows, and its plan, to device memory

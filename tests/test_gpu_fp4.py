@@ -84,6 +84,44 @@ def test_products_of_many_shapes(m, n, k, gated):
     product_case(m, n, k, gated)
 
 
+@pytest.mark.parametrize("m,n,k,gated", [(100, 14336, 544, True), (160, 14416, 288, True), (200, 14320, 800, True), (12, 10256, 4096, False),
+                                         (5, 10256, 1056, False), (16, 1040, 14336, True), (300, 4112, 14336, False), (13, 2064, 14304, False),
+                                         (65, 10256, 8288, False), (16, 14416, 1312, True), (2, 6160, 4096, False), (3, 6160, 4096, True)])
+def test_products_of_every_cut(m, n, k, gated):
+    """Tiles of one to seven, kernels for few and many rows, whole and in slices, columns that end inside a unit or a chunk."""
+    product_case(m, n, k, gated)
+
+
+@pytest.mark.parametrize("m,n", [(1, 4096), (12, 1024), (30, 4096), (64, 4096), (100, 28672), (150, 28672), (200, 28672)])
+def test_columns_past_the_end_count_as_nothing(m, n):
+    """Storage goes on to a multiple of 256 columns.  Whatever was in shared memory before: here NaN, out of a product before."""
+    x, w = rnd(m, m, 1056), rnd(n, n, 1056, scale=0.05)
+    nan = torch.full((m, 1056), float("nan"), dtype=torch.bfloat16, device="cuda")
+    full = sp.fp4_pack_matrix(w)
+    for k in (32, 160, 288, 1056):
+        xk, p = x[:, :k].contiguous(), sp.fp4_pack_matrix(w[:, :k].contiguous())
+        first = sp.fp4_product(xk, p)
+        assert torch.isfinite(first).all()
+        assert torch.isnan(sp.fp4_product(nan, full)).all()
+        assert torch.equal(sp.fp4_product(xk, p), first)
+
+
+def test_a_gated_product_of_a_matrix_past_2_gb():
+    """Gate and up rows more than 2 GB apart: one strip of both is not zero."""
+    n, k = 65536, 131072
+    units = k // 256
+    w = sp.Fp4Matrix(torch.zeros(sp.load_library().sp_fp4_matrix_bytes(2 * n, k), dtype=torch.uint8, device="cuda"), 2 * n, k)
+    gate, up, x = rnd(1, 16, k, scale=0.02), rnd(2, 16, k, scale=0.02), rnd(3, 3, k)
+    at = [s * units * 2176 for s in (n // 16 - 1, 2 * n // 16 - 1)]
+    for part, o in zip((gate, up), at):
+        piece = sp.fp4_pack_matrix(part).data
+        w.data[o:o + piece.numel()] = piece
+    y = f64(sp.fp4_product(x, w, gated=True))
+    assert not y[:, :n - 16].any()
+    small = sp.fp4_pack_matrix(torch.cat([gate, up]))
+    assert np.allclose(y[:, n - 16:], f64(sp.fp4_product(x, small, gated=True)), rtol=2.0 ** -7, atol=2.0 ** -7)
+
+
 def test_a_row_that_is_not_finite_stays_alone():
     """Columns are padded to 256 in storage; what lies behind a row of x is the next row, here NaN and infinity."""
     for m in (3, 20, 70):
