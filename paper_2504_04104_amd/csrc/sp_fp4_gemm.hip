@@ -9,8 +9,8 @@
 //
 // Two kernels: up to 16 rows of short products the waves of a workgroup share strips and cut the columns among them; elsewhere
 // they have strips of their own and share rows of X through LDS.  What bounds them: up to some forty rows the weights' way from
-// memory (28672 x 4096, 62 MB: one row 11.0 us, 5.7 TB/s; 28672 wide twice, 8192 deep, 249 MB: 44.6 us); more rows the matrix
-// cores' feeding, 200 rows of the last 172 us, 1.09 PFLOP/s.
+// memory (one row of 28672 x 4096, 62 MB, 14.6 us; of 57344 x 8192, 249 MB, 45.9 us, 5.4 TB/s); more rows, the rows' way through
+// L2 and LDS into the matrix cores (64 rows of 28672 x 4096 20.4 us; 200 rows of 57344 x 8192 170 us, 1.1 PFLOP/s).
 #include "sp_launch.h"
 #include "sp_fp4.h"
 
@@ -125,14 +125,14 @@ __global__ void __launch_bounds__(NS <= 2 ? 512 : 256) k_fp4_few(Fp4GemmArgs a) 
 }
 
 // The waves share the rows of X through LDS, which a load brings there without registers, and have NS strips each over all columns
-// of the slice.  A chunk is 128 columns, half a unit; loads are three chunks ahead, a chunk's rows before its weights, and go out
-// between the products: all at once behind the barrier they held up the matrix cores (4096 x 14336, 64 rows, four tiles and four
-// strips whole 91.8 us, 83.3 between).
-#define CHUNKS_AHEAD 3
+// of the slice.  A chunk is 128 columns, half a unit; loads are three chunks ahead (five are no faster), a chunk's rows before its
+// weights, and go out between the products: all at once behind the barrier they held up the matrix cores (4096 x 14336, 64 rows,
+// four tiles and four strips whole 91.8 us, 83.3 between).
 #define PANELS 4
+#define AHEAD 3
 template <int MT, int NS, int OUT>
 __global__ void __launch_bounds__(256, MT * NS <= 16 ? 2 : 1) k_fp4_many(Fp4GemmArgs a) {
-  constexpr int PANEL = MT * 4096;
+  constexpr int PANEL = MT * 4096, LOADS = MT + 2 * NS;
   // arrays of their own, so that the compiler knows which loads a read has to wait for
   __shared__ __attribute__((aligned(16))) char p0[PANEL];
   __shared__ __attribute__((aligned(16))) char p1[PANEL];
@@ -159,13 +159,20 @@ __global__ void __launch_bounds__(256, MT * NS <= 16 ? 2 : 1) k_fp4_many(Fp4Gemm
     live[i] = strip0 + i % own < (OUT == OUT_GATED ? strips >> 1 : strips) ? strip_bytes : 0;
     w[i] = a.W + (live[i] ? (size_t)strip * strip_bytes : 0);
   }
-  // A load to LDS brings a tile's 16 rows x 32 columns, lane (l15, kg) 16 bytes of row l15: a kilobyte of X in fragment order, or
-  // 64 bytes of each row where they lie one after the other.  Rows past the last are past the buffer's end.
-  const int xk = a.frag ? a.units * UNIT_K : a.K, k_step = a.frag ? 1024 : 64, lane16 = lane * 16;
-  const int x_rows = min(a.M - t0 * 16, MT * 16), x_bytes = (a.frag ? (x_rows + 15) & ~15 : x_rows) * xk * 2, x_blocks = min(xk >> 5, c_end * 4);
+  // A load to LDS brings eight rows x 64 columns of a tile, the wave's of its four: lane l 16 bytes (a piece) of row l / 8.  They
+  // are whole lines of X, row-major or in fragment order (64 rows of 28672 x 4096 21.7 us, by 32 columns of 16 rows 23.3).  The
+  // pieces of a row are exchanged by the row's number, for reads without bank conflicts.  Rows past the last, and columns (of the
+  // last chunk) past the end, are past the buffer's end: zeros.
+  const int r8 = lane >> 3, piece = (lane & 7) ^ r8 ^ (wave & 1), x_row = (wave & 1) * 8 + r8, x_col = (wave >> 1) * 64 + piece * 8;
+  const int xk = a.frag ? a.units * UNIT_K : a.K, x_step = a.frag ? 4096 : 256;
+  const int x_rows = min(a.M - t0 * 16, MT * 16), x_bytes = (a.frag ? (x_rows + 15) & ~15 : x_rows) * xk * 2;
   const bf16_t* xblk = a.X + (size_t)t0 * 16 * xk;
-  const int x_lane = a.frag ? lane16 : l15 * xk * 2 + kg * 16;
-
+  const int x_lane = a.frag ? (x_col >> 5) * 1024 + (piece & 3) * 256 + x_row * 16 : (x_row * xk + x_col) * 2;
+  const int c_part = a.K % 128 ? a.K / 128 : -1, x_part = x_col < a.K % 128 ? x_lane : 0x7fffff00;
+  const int lane16 = lane * 16;
+  int read_at[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) read_at[j] = ((kg >> 1) * 2 + (l15 >> 3)) * 1024 + (l15 & 7) * 128 + (((kg & 1) * 4 + j) ^ (l15 & 7) ^ (l15 >> 3)) * 16;
   // the word with the lane's two scales, and the turn that brings the first into the exponent field
   const int scale_at = 2048 + (lane & 62) * 2, turn = (lane & 1) * 16 + 9;
   u32x4_t wb[PANELS][NS];
@@ -177,10 +184,10 @@ __global__ void __launch_bounds__(256, MT * NS <= 16 ? 2 : 1) k_fp4_many(Fp4Gemm
     for (int i = 0; i < NS; ++i) acc[t][i] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
 #define SP_LOAD_X(I, C)                                                                                                \
   {                                                                                                                    \
-    const int k_ = (C) * 4 + wave;                                                                                     \
-    const auto xb_ = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(xblk), (short)0, k_ < x_blocks ? x_bytes : 0, 0x00020000); \
+    const auto xb_ = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(xblk), (short)0, (C) < c_end ? x_bytes : 0, 0x00020000); \
+    const int x_ = (C) == c_part ? x_part : x_lane;                                                                    \
     _Pragma("unroll") for (int t = 0; t < MT; ++t)                                                                     \
-        load_to_lds(xb_, SP_PAN(I) + (t * 4 + wave) * 1024, x_lane + t * 32 * xk, k_ * k_step);                        \
+        load_to_lds(xb_, SP_PAN(I) + (t * 4 + wave) * 1024, x_ + t * 32 * xk, (C) * x_step);                           \
   }
 #define SP_LOAD_W(I, C, s)                                                                                             \
   {                                                                                                                    \
@@ -190,7 +197,7 @@ __global__ void __launch_bounds__(256, MT * NS <= 16 ? 2 : 1) k_fp4_many(Fp4Gemm
   }
 #define SP_READ(I, j, Q)                                                                                               \
   _Pragma("unroll") for (int t = 0; t < MT; ++t)                                                                       \
-      xq[Q][t] = *reinterpret_cast<const u32x4_t*>(SP_PAN(I) + t * 4096 + kg * 1024 + (j) * 256 + l15 * 16);
+      xq[Q][t] = *reinterpret_cast<const u32x4_t*>(SP_PAN(I) + t * 4096 + read_at[j]);
   // A quarter of a chunk's products, between them the reads for the next quarter and a part of the loads
 #define SP_STEP(I, j, LOADS)                                                                                           \
   {                                                                                                                    \
@@ -213,29 +220,29 @@ __global__ void __launch_bounds__(256, MT * NS <= 16 ? 2 : 1) k_fp4_many(Fp4Gemm
   }
 #define SP_CHUNK(I, C)                                                                                                 \
   {                                                                                                                    \
-    SP_WAIT_VMEM(MT + 2 * 2 * NS);                                                                                     \
+    SP_WAIT_VMEM((AHEAD - 2) * LOADS + 2 * NS);                                                                        \
     bare_barrier();                                                                                                    \
-    const int ahead_ = (C) + CHUNKS_AHEAD;                                                                             \
-    SP_STEP(I, 0, SP_LOAD_X(((I) + CHUNKS_AHEAD) % PANELS, ahead_))                                                    \
-    SP_STEP(I, 1, _Pragma("unroll") for (int s = 0; s < NS; s += 2) SP_LOAD_W(((I) + CHUNKS_AHEAD) % PANELS, ahead_, s)) \
-    SP_STEP(I, 2, _Pragma("unroll") for (int s = 1; s < NS; s += 2) SP_LOAD_W(((I) + CHUNKS_AHEAD) % PANELS, ahead_, s)) \
+    const int ahead_ = (C) + AHEAD;                                                                             \
+    SP_STEP(I, 0, SP_LOAD_X(((I) + AHEAD) % PANELS, ahead_))                                                    \
+    SP_STEP(I, 1, _Pragma("unroll") for (int s = 0; s < NS; s += 2) SP_LOAD_W(((I) + AHEAD) % PANELS, ahead_, s)) \
+    SP_STEP(I, 2, _Pragma("unroll") for (int s = 1; s < NS; s += 2) SP_LOAD_W(((I) + AHEAD) % PANELS, ahead_, s)) \
     SP_STEP(I, 3, )                                                                                                    \
   }
 #define SP_CHUNK_PRODUCTS(I) { SP_STEP(I, 0, ) SP_STEP(I, 1, ) SP_STEP(I, 2, ) SP_STEP(I, 3, ) }
 #pragma unroll
-  for (int p = 0; p < CHUNKS_AHEAD; ++p) {
+  for (int p = 0; p < AHEAD; ++p) {
     SP_LOAD_X(p, c_begin + p)
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int s = 0; s < NS; ++s) SP_LOAD_W(p, c_begin + p, s)
     __builtin_amdgcn_sched_barrier(0);
   }
-  SP_WAIT_VMEM(2 * (MT + 2 * NS) + 2 * NS);
+  SP_WAIT_VMEM((AHEAD - 1) * LOADS + 2 * NS);
   bare_barrier();
   u32x4_t xq[2][MT];
   SP_READ(0, 0, 0)
   int c = c_begin;
-  for (; c + 4 <= c_end; c += 4) {
+  for (; c + PANELS <= c_end; c += PANELS) {
     SP_CHUNK(0, c)
     SP_CHUNK(1, c + 1)
     SP_CHUNK(2, c + 2)
@@ -364,17 +371,18 @@ hipError_t sp_launch_fp4_unpack(const void* in, void* out, int N, int K, hipStre
 
 // How a product is cut: tiles of rows (0: the kernel for few rows) and strips of a workgroup, and slices of the columns, whose
 // sums are joined by a launch of their own (`join` us; 0 where whoever takes the partial sums adds them up).  What is least by
-// these times, which are those of a chunk of 128 columns with one workgroup on a CU, in 112 chunks: 0.21 us for one tile and two
-// strips, 0.27 for two tiles, 0.46 and 0.70 for four with two and four strips, 0.93 for five, 1.22 for seven; a unit of a wave of
-// the kernel for few rows 1 us and more with every row; a megabyte of partial sums 0.3.  Workgroups past the CUs take turns: two
-// at a time on a CU are not faster than one after the other.  Us a call as chosen, and next to it: 64 rows, 28672 x 4096 gated,
-// tiles x strips 4 x 2 20.3 (2 x 2 22.1, 4 x 4 26.8), 100 rows 4 x 4 27.3 (4 x 2 37.0), 160 rows 5 x 4 35.1 (4 x 4 46.8), 200 rows
-// 7 x 4 44.2 (4 x 4 48.5), 256 rows 4 x 4 50.6 (7 x 4 85.1); 4096 x 14336, 17 rows 2 x 2 in 8 slices 12.4 (in 4 13.9, whole 33.3),
-// 64 rows in 4 14.8 (in 8 16.8), 200 rows 4 x 4 in 4 30.9 (2 x 2 whole 35.0); one row, 4096 x 4096 with the kernel for few rows 6.8
-// (one tile in 4 slices 9.7), 4096 x 14336 with one tile in 8 slices 10.8 (few rows' 11.4), 28672 x 4096 gated 11.0 (few rows' 15.7).
+// these times: a chunk of 128 columns, of 112 with at most one workgroup on a CU, 0.25 us for one tile and two strips, 0.28 for
+// two tiles, 0.40 and 0.66 for four with two and four strips, 0.82 for five, 1.12 for seven; a unit of a wave of the kernel for
+// few rows 1 us and more with every row; a megabyte of partial sums 0.3.  Workgroups past the CUs take turns: two at a time on a
+// CU are not faster than one after the other.  Us a call, as chosen and next to it (tiles x strips): 28672 x 4096 gated, 64 rows
+// 4 x 2 20.4 (2 x 2 23.9, 4 x 4 27.4), 100 rows 4 x 4 29.3 (4 x 2 30.9), 160 rows 5 x 4 36.7 (4 x 4 45.2), 200 rows 7 x 4 46.4
+// (4 x 4 47.9), 256 rows 4 x 4 51.7 (7 x 4 84.2); 4096 x 14336, 17 rows 2 x 2 in 8 slices 13.2 (in 4 15.2, whole 35.8), 64 rows
+// in 4 16.2 (in 8 18.0), 200 rows 4 x 4 in 4 31.9 (2 x 2 whole 37.5); with the kernel for few rows, 4096 x 4096, one row 7.5 (one
+// tile whole 10.1, in 4 slices 11.8), 16 rows 8.5 (10.4); 4096 x 14336, one row 11.7 (one tile in 8 slices 12.0), nine 14.8 (12.6);
+// 28672 x 4096 gated, one row with one tile 14.6 (few rows' 15.9), 16 rows 15.0 (19.9).
 struct Fp4Split { int mt, ns, S; };
 static Fp4Split split_of(int M, int N, int K, int n_cu, float join, int most_slices) {
-  static const struct { int mt, ns; float us; } tiled[] = {{1, 2, .21f}, {2, 2, .27f}, {4, 2, .46f}, {4, 4, .70f}, {5, 4, .93f}, {7, 4, 1.22f}};
+  static const struct { int mt, ns; float us; } tiled[] = {{1, 2, .25f}, {2, 2, .28f}, {4, 2, .40f}, {4, 4, .66f}, {5, 4, .82f}, {7, 4, 1.12f}};
   static const struct { int ns, waves; float us, us_row; } few[] = {{1, 8, 1.f, .07f}, {2, 8, 1.6f, .06f}, {4, 4, 1.f, .06f}};
   const int units = (K + UNIT_K - 1) / UNIT_K, strips = N / 16;
   Fp4Split best = {0, 1, 1};
@@ -394,7 +402,7 @@ static Fp4Split split_of(int M, int N, int K, int n_cu, float join, int most_sli
   }
   return best;
 }
-#define JOIN_US 3.5f
+#define JOIN_US 6.f
 #define MOST_SLICES 16
 size_t sp_fp4_product_floats(int M, int N, int K, int n_cu) {
   const Fp4Split f = split_of(M, N, K, n_cu, JOIN_US, MOST_SLICES);
