@@ -315,7 +315,7 @@ int sp_stage_forward(sp_stage* stage, int32_t n_req, const int32_t* req_ids /*ho
 /* The attention of one layer piece by piece, for layers whose other parts the caller computes (its own projections or mixing):
  * the same rows, order and errors as sp_stage_forward, plus SP_E_INVALID for a layer outside the stage.
  * sp_stage_append takes the rows of the QKV projection, [sum n_nodes][(n_q + 2 n_kv) * d_head] in the config dtype (query
- * heads, key heads, value heads): norms of the query and key heads where the stage has them, rotation at prefix_len + depth,
+ * heads, key heads, value heads), which q_out may not overlap: norms of the query and key heads where the stage has them, rotation at prefix_len + depth,
  * K and V into the nodes' cache slots, the queries to q_out [sum n_nodes][n_q * d_head], in one launch.  Appending to the
  * stage's last layer makes the nodes count as forwarded.
  * sp_stage_attention computes the tree attention of such queries over what the layer's cache holds: softmax(q K^T /

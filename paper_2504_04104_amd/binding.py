@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import array
 import ctypes as C
+import functools
 import os
 from typing import Dict, List, Optional, Sequence
 
@@ -703,7 +704,9 @@ def fp4_pack_weights(shape, layers: List[Dict[str, "object"]]):
     return out
 
 
-_workspace_bytes: Dict[tuple, int] = {}          # of products, by their sizes and device
+@functools.lru_cache(4096)
+def _workspace_bytes(m: int, n: int, k: int, gated: int, device: int) -> int:
+    return load_library().sp_fp4_product_workspace(m, n, k, gated)      # (of the current device)
 
 
 def fp4_product(x, w: Fp4Matrix, gated: bool = False, out=None):
@@ -712,6 +715,7 @@ def fp4_product(x, w: Fp4Matrix, gated: bool = False, out=None):
     import torch
     lib = load_library()
     device = x.device
+    assert x.is_cuda and w.data.device == device
     if device.index != torch._C._cuda_getDevice():
         with torch.cuda.device(device):
             return fp4_product(x, w, gated, out)
@@ -720,15 +724,12 @@ def fp4_product(x, w: Fp4Matrix, gated: bool = False, out=None):
         if n % 32:
             raise SpError(-9, "a gated product of %d rows" % n)
         n //= 2
-    assert x.is_cuda and x.dtype is torch.bfloat16 and x.dim() == 2 and x.shape[1] == k and x.is_contiguous()
+    assert x.dtype is torch.bfloat16 and x.dim() == 2 and x.shape[1] == k and x.is_contiguous()
     if out is None:
         out = torch.empty(m, n, dtype=torch.bfloat16, device=device)
     else:
         assert out.device == device and out.dtype is torch.bfloat16 and out.shape == (m, n) and out.is_contiguous()
-    key = (m, n, k, gated, device.index)
-    size = _workspace_bytes.get(key)
-    if size is None:
-        size = _workspace_bytes[key] = lib.sp_fp4_product_workspace(m, n, k, int(gated))
+    size = _workspace_bytes(m, n, k, int(gated), device.index)
     work = torch.empty(size, dtype=torch.uint8, device=device) if size else None
     _check(lib.sp_fp4_product(x.data_ptr(), m, w.data.data_ptr(), n, k, 1 if gated else 0, out.data_ptr(), work.data_ptr() if size else None,
                               size, torch._C._cuda_getCurrentRawStream(device.index)), "sp_fp4_product")

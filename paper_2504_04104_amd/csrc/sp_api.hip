@@ -439,6 +439,9 @@ int sp_pack_matrix(const void* in, void* out, int32_t n_rows, int32_t n_cols, sp
 }
 
 // ---- 4-bit weights --------------------------------------------------------------------------------
+static bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
+  return (uintptr_t)a < (uintptr_t)b + b_bytes && (uintptr_t)b < (uintptr_t)a + a_bytes;
+}
 static bool fp4_shape(int64_t n_rows, int64_t n_cols) {
   return n_rows >= 16 && n_cols >= 32 && n_rows % 16 == 0 && n_cols % 32 == 0 && n_rows <= SP_FP4_MAX_DIM && n_cols <= SP_FP4_MAX_DIM;
 }
@@ -495,6 +498,7 @@ int sp_fp4_product(const void* x, int32_t m, const void* w, int32_t n, int32_t k
   if (m > SP_FP4_MAX_DIM || !fp4_shape((int64_t)n << gated, k) || n % 16) return SP_E_UNSUPPORTED;
   if (m == 0) return SP_OK;
   if (!x || !w || !out || (((uintptr_t)x | (uintptr_t)w | (uintptr_t)out | (uintptr_t)workspace) & 15)) return SP_E_INVALID;
+  if (overlap(x, (size_t)m * k * 2, out, (size_t)m * n * 2)) return SP_E_INVALID;
   const size_t need = sp_fp4_product_workspace(m, n, k, gated);
   if (need > 0 && (!workspace || workspace_bytes < need)) return SP_E_CAPACITY;
   return sp_launch_fp4_product((const bf16_t*)x, w, gated != 0, (bf16_t*)out, (float*)workspace, m, n << gated, k, current_cus(),
@@ -1008,6 +1012,8 @@ int sp_stage_append(sp_stage* s, int32_t layer, int32_t n_req, const int32_t* re
   if (layer < 0 || layer >= c.n_layers) return SP_E_INVALID;
   if (b.n_rows == 0) return SP_OK;
   if (!qkv || !q_out || (((uintptr_t)qkv | (uintptr_t)q_out) & 15)) return SP_E_INVALID;
+  const size_t head_rows = (size_t)b.n_rows * c.d_head * elt_bytes(c.dtype);
+  if (overlap(qkv, head_rows * (c.n_q_heads + 2 * c.n_kv_heads), q_out, head_rows * c.n_q_heads)) return SP_E_INVALID;
   const bool normed = !s->norms.empty();
   { ProfScope p(s, SP_K_ROPE_KV, (hipStream_t)stream);
     const hipError_t e = sp_launch_append_rows(c.dtype, qkv, b, s->d_meta, s->d_tables, std::log2((double)c.rope_theta),
@@ -1026,7 +1032,9 @@ int sp_stage_attention(sp_stage* s, int32_t layer, int32_t n_req, const int32_t*
   const sp_config& c = s->cfg;
   if (layer < 0 || layer >= c.n_layers) return SP_E_INVALID;
   if (b.n_rows == 0) return SP_OK;
-  if (!q || !out || q == out || (((uintptr_t)q | (uintptr_t)out) & 15)) return SP_E_INVALID;
+  if (!q || !out || (((uintptr_t)q | (uintptr_t)out) & 15)) return SP_E_INVALID;
+  const size_t q_bytes = (size_t)b.n_rows * c.n_q_heads * c.d_head * elt_bytes(c.dtype);
+  if (overlap(q, q_bytes, out, q_bytes)) return SP_E_INVALID;
   hipStream_t st = (hipStream_t)stream;
   const Workspace& w = s->ws;
   const int M = b.n_rows, nq = c.n_q_heads, nkv = c.n_kv_heads, dh = c.d_head;
@@ -1071,7 +1079,8 @@ int sp_kv_store(sp_stage* s, int32_t req, int32_t layer, int32_t first_slot, int
 int sp_kv_load(sp_stage* s, int32_t req, int32_t layer, int32_t first_slot, int32_t n, void* k, void* v, sp_stream stream) {
   const int rc = check_slots(s, req, layer, first_slot, n, k, v);
   if (rc != SP_OK || n == 0) return rc;
-  if (k == v) return SP_E_INVALID;
+  const size_t bytes = (size_t)n * s->cfg.n_kv_heads * s->cfg.d_head * elt_bytes(s->cfg.dtype);
+  if (overlap(k, bytes, v, bytes)) return SP_E_INVALID;
   const hipError_t e = sp_launch_kv_load(s->cfg.dtype, s->geom, req, s->reqs[req].base, layer, first_slot, n, k, v, s->cfg.n_kv_heads,
                                          s->cfg.d_head, (hipStream_t)stream);
   return e == hipSuccess ? SP_OK : hip_fail(s, e);

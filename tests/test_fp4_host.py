@@ -48,7 +48,7 @@ def test_bytes_of_packed_matrices():
 
 def test_refused_products_and_matrices():
     lib = sp.load_library()
-    p = [C.c_void_p(4096 * (i + 1)) for i in range(4)]                 # never read: every call below is refused first
+    p = [C.c_void_p((i + 1) << 24) for i in range(4)]                  # never read: every call below is refused first
     odd = C.c_void_p(4104)
 
     def product(x=p[0], m=1, w=p[1], n=16, k=32, gated=0, out=p[2], work=None, size=0):
@@ -59,9 +59,11 @@ def test_refused_products_and_matrices():
         assert product(**bad) == INVALID, bad
     for bad in (dict(n=17), dict(k=48), dict(n=8, gated=1), dict(n=1 << 17, gated=1), dict(k=1 << 18), dict(m=(1 << 17) + 1), dict(n=2 ** 31 - 16)):
         assert product(**bad) == UNSUPPORTED, bad
-    need = lib.sp_fp4_product_workspace(1, 16, 8192, 0)
+    for out in (1 << 24, (1 << 24) + 4 * 64 - 16, (1 << 24) - 4 * 32 + 16):        # rows of x, or of the result, in the other's
+        assert product(m=4, out=C.c_void_p(out)) == INVALID
+    need = lib.sp_fp4_product_workspace(64, 16, 8192, 0)                # columns cut, sums joined
     assert need > 0
-    assert product(k=8192) == CAPACITY and product(k=8192, work=p[3], size=need - 1) == CAPACITY
+    assert product(m=64, k=8192) == CAPACITY and product(m=64, k=8192, work=p[3], size=need - 1) == CAPACITY
     assert product(m=0) == OK
     assert lib.sp_fp4_product_workspace(1, 17, 32, 0) == 0 and lib.sp_fp4_product_workspace(-1, 16, 32, 0) == 0
     for f in (lib.sp_fp4_pack_matrix, lib.sp_fp4_unpack_matrix):

@@ -438,6 +438,10 @@ def test_refusals_leave_the_stage_as_it_was():
     refused(-5, lambda: st.attention(0, [0], [1], [4], q))
     refused(-1, lambda: st.attention(0, [0], [0], [4], q, q))
     refused(-1, lambda: st.attention(0, [0, 0], [0, 0], [2, 2], q))
+    both = torch.zeros(7, 1024, dtype=torch.bfloat16, device="cuda")
+    refused(-1, lambda: st.attention(0, [0], [0], [4], both[:4], both[3:]))
+    wide = torch.zeros(4 * 12 * 128, dtype=torch.bfloat16, device="cuda")
+    refused(-1, lambda: st.append(0, [0], [0], [4], wide.view(4, -1), wide[:4096].view(4, -1)))
     refused(-2, lambda: st.kv_load(0, 0, 40, 5))
     refused(-1, lambda: st.kv_load(0, 0, -1, 2))
     refused(-1, lambda: st.kv_load(0, 2, 0, 2))
@@ -458,6 +462,33 @@ def test_refusals_leave_the_stage_as_it_was():
         sp.fp4_pack_matrix(rnd(1, 17, 64))
     with pytest.raises(sp.SpError):
         sp.fp4_product(rnd(1, 2, 64), sp.fp4_pack_matrix(rnd(1, 48, 64)), gated=True)
+    square, room = sp.fp4_pack_matrix(rnd(1, 64, 64)), torch.zeros(5, 64, dtype=torch.bfloat16, device="cuda")
+    refused(-1, lambda: sp.fp4_product(room[:3], square, out=room[2:]))
+    with pytest.raises(AssertionError):
+        sp.fp4_product(room.cpu(), square)
+
+
+def test_a_cache_past_32_bits():
+    """A slab of 5 GB: the last heads' codes and scales lie past 4 GB, the last request's slots past 2^32 bytes of its planes' start."""
+    sh, slots = shape(8, 8, 128), 4600 * 1000
+    st = stage(sp, sh, slots=slots, flags=sp.SP_FLAG_FP4_KV, requests=2)
+    P = 500
+    for i, base in enumerate((0, slots - 600)):
+        st.request_init(i, base, 600, P)
+        st.tree_insert(i, [-1, 0])
+        k, v = rnd(10 + i, P, 8, 128), rnd(20 + i, P, 8, 128)
+        st.kv_store(i, 0, 0, k, v)
+        qkv = rnd(30 + i, 2, 24 * 128)
+        q = st.append(0, [i], [0], [2], qkv)
+        out = st.attention(0, [i], [0], [2], q)
+        hk, hv = (f64(t) for t in st.kv_load(i, 0, 0, P + 2))
+        assert np.array_equal(hk[:P], held(f64(k))) and np.array_equal(hv[:P], held(f64(v)))
+        assert np.array_equal(hv[P:], held(f64(qkv[:, 16 * 128:]).reshape(2, 8, 128)))
+        seen = np.ones((2, P + 2), bool)
+        seen[0, P + 1] = False
+        y, mag, big = attend(f64(q).reshape(2, 8, 128), hk, hv, seen)
+        off = U * np.abs(y) + (1.01 * U + (8 + 256) * F * (1 + big[..., None]) + 64 * F) * mag
+        assert (np.abs(f64(out).reshape(y.shape) - y) <= off).all()
 
 
 # ---- the whole stage ---------------------------------------------------------------------------------------------------
