@@ -8,8 +8,8 @@
 //
 // A head belongs to d_head / 8 consecutive lanes, a lane holds four pairs: columns t .. t+3 and d_head/2 + t .. + 3.  Sums over
 // the head and maxima over the eight lanes of a 4-bit group stay in the wave; nothing goes through LDS but the angles' sines.
-// Everything is float32 until the one rounding to the storage type.  Bound by the launch for a tree level (5 us for 1 to 64
-// rows), by the rows' bytes for several hundred.
+// Everything is float32 until the one rounding to the storage type.  Bound by the launch and a chain of lookups (request,
+// its prefix, the node's depth, its page) for a tree level: one row 3.6 us, 64 rows 4.2; 640 rows, 16 MB, 6.8.
 #include "sp_launch.h"
 #include "sp_fp4.h"
 
@@ -106,22 +106,27 @@ __global__ void __launch_bounds__(256) k_head_append(AppendArgs a, FwdBatch b) {
     load4(gain + half + t, gv);
   }
 
-  int req, node, P;
-  long long base;
+  size_t slot;
   const float* cs;
   if constexpr (PART) {
     const RowInfo ri = a.rows[row];
-    req = ri.req; node = ri.node; P = ri.P; base = ri.base;
+    slot = sp_phys_slot(a.g, ri.req, ri.base, ri.P + ri.node);
     cs = a.cs + (size_t)row * a.d_head;
   } else {
+    // Few requests one after the other, many a lane each (640 rows of 32 requests 10.0 us one after the other, 6.8; one request 3.6
+    // and, a lane each, 3.9).
+    static_assert(SP_BATCH <= 64, "a lane per request");
+    const int lane = threadIdx.x & 63;
     int seg = 0;
-    while (seg + 1 < b.n_req && row >= b.row0[seg + 1]) ++seg;
-    req = b.req[seg]; node = b.first[seg] + (row - b.row0[seg]);
+    if (b.n_req > 4) seg = __popcll(__builtin_amdgcn_ballot_w64(lane < b.n_req && row >= b.row0[lane])) - 1;
+    else while (seg + 1 < b.n_req && row >= b.row0[seg + 1]) ++seg;
+    const int req = b.req[seg], node = b.first[seg] + (row - b.row0[seg]);
     const ReqMeta m = a.meta[req];
-    P = m.P; base = m.base;
+    const int depth = a.tables[req].depth[node];
+    slot = sp_phys_slot(a.g, req, m.base, m.P + node);
     // The angle in double precision, whole turns taken off there: positions of tens of thousands keep full float accuracy.
     if ((int)threadIdx.x < half) {
-      const double pos = (double)(P + a.tables[req].depth[node]);
+      const double pos = (double)(m.P + depth);
       const double turns = pos * exp2(-(2.0 * (double)threadIdx.x / (double)a.d_head) * a.log2_theta) * 0.15915494309189535;
       const float ang = (float)((turns - rint(turns)) * 6.283185307179586);
       s_cs[threadIdx.x] = cosf(ang);
@@ -159,7 +164,7 @@ __global__ void __launch_bounds__(256) k_head_append(AppendArgs a, FwdBatch b) {
   } else {
     const bool is_v = head >= a.n_q + a.n_kv;
     const size_t plane = (size_t)(a.layer * 2 + (is_v ? 1 : 0)) * a.n_kv + (head - a.n_q - (is_v ? a.n_kv : 0));
-    put_row<T, FP4>(a.g, plane, sp_phys_slot(a.g, req, base, P + node), half, t, u, v);
+    put_row<T, FP4>(a.g, plane, slot, half, t, u, v);
   }
 }
 
