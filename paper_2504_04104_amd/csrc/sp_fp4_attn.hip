@@ -179,8 +179,12 @@ __device__ __forceinline__ void attn_fp4(const Fp4AttnArgs& a, const AttnPlan& p
   const int nqrows = seg_rows * g;                 // query rows of this (request, KV head): node * g + head of the group
   const int c0 = ch * clen, c1 = min(c0 + clen, span);
   const int ntiles = (c1 - c0 + 31) >> 5;
-  const int w0 = c0 + 32 * ((wave * ntiles) / NW);
-  const int w1 = min(c0 + 32 * (((wave + 1) * ntiles) / NW), c1);
+  // Waves 4 to 7 share their SIMDs with waves 0 to 3, which go first: where blocks share a range and nothing else is waited for,
+  // tiles take them 0.85 us and 0.6, and they get 14 for every 18 (64 rows behind 16000 slots 33.2 -> 31.8 us, 128 behind 8000
+  // 27.5 -> 26.1; ranges that a block streams for itself 18.6 -> 19.4, even shares).  Tiles left over go to the first waves.
+  const int share = plan.seg_qblocks[seg] > 1 ? 18 : 16;
+  auto first_tile = [&](int w) { return (ntiles * (w <= 4 ? w * share : 4 * share + (w - 4) * (32 - share)) + 127) >> 7; };
+  const int w0 = c0 + 32 * first_tile(wave), w1 = min(c0 + 32 * first_tile(wave + 1), c1);
 
   // The query rows are asked for first, then the first tile: what is waited for comes in this order.
   const float inv_g = __uint_as_float(uni(__float_as_uint(__builtin_amdgcn_rcpf((float)g))));               // (qi + 0.5) * inv_g truncates to qi / g for these small integers
