@@ -995,9 +995,13 @@ int sp_stage_set_head_norms(sp_stage* s, const sp_head_norms* layers) {
       if (!layers[l].q || !layers[l].k) return SP_E_INVALID;
       if (((uintptr_t)layers[l].q | (uintptr_t)layers[l].k) & 15) return SP_E_INVALID;
     }
+  // what was captured does not know these pointers (and may be running)
+  if (!s->graphs.empty()) {
+    const hipError_t e = hipDeviceSynchronize();
+    if (e != hipSuccess) return hip_fail(s, e);
+  }
   if (layers) s->norms.assign(layers, layers + s->cfg.n_layers);
   else s->norms.clear();
-  // what was captured does not know these pointers
   for (auto& g : s->graphs) if (g.exec) (void)hipGraphExecDestroy(g.exec);
   s->graphs.clear();
   return SP_OK;

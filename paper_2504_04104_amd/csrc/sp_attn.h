@@ -1,17 +1,7 @@
-// What the attention kernels have in common: the transposing reads of a V tile, and the merge of ranges that were cut into
-// chunks.
+// What the attention kernels have in common: the merge of ranges that were cut into chunks.
 #pragma once
 #include "sp_launch.h"
 
-// Sixteen lanes read four slots x 16 columns, lane 4c + x of them gets the four slots of one column.
-typedef __attribute__((ext_vector_type(4))) short s16x4_t;
-__device__ __forceinline__ uint2 read_transposed(const char* p) {
-#ifdef __HIP_DEVICE_COMPILE__
-  return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(p)));
-#else
-  return uint2{0u, 0u};
-#endif
-}
 // One wave per (row, query head) of the requests that were cut into several chunks: combine the
 // chunk partials (log2-domain maxima).  Lane c first takes chunk c's (max, sum) and turns them into
 // the chunk's weight; the outputs are then accumulated chunk by chunk, two columns per lane.

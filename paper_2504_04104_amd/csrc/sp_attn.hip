@@ -139,6 +139,14 @@ __device__ __forceinline__ void attn_softmax(AttnState<QT>& st, const f32x4_t (&
 
 // O^T += V^T P^T; va: the lane's places for the transposing reads.  Sixteen lanes read four slots x 16 columns, lane 4c + x of
 // them gets the four slots of column G*32 + 8c + 4e + x, and so a lane's products of e = 0 and 1 are eight columns in a row.
+typedef __attribute__((ext_vector_type(4))) short s16x4_t;
+__device__ __forceinline__ uint2 read_transposed(const char* p) {
+#ifdef __HIP_DEVICE_COMPILE__
+  return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(p)));
+#else
+  return uint2{0u, 0u};
+#endif
+}
 template <int QT>
 __device__ __forceinline__ void attn_pv(AttnState<QT>& st, const uint32_t (&pb)[QT][4], const char* vt, const int (&va)[4]) {
 #pragma unroll

@@ -1,11 +1,10 @@
 // Values held in 4 bits (e2m1: sign, two exponent bits, one mantissa bit) with one power of two for 32 of them.
 //
 // A group's scale is 2^e for the smallest e in [-100, 125] with max |x| <= 6 * 2^e, stored as e + 127; a value is
-// +-{0, 0.5, 1, 1.5, 2, 3, 4, 6} * 2^e, rounded to nearest with ties to the even code: off by at most a quarter of its group's
-// largest value's own power of two, 6 / 2 = 3 being half a step of the widest gap.  All of it is exact in bfloat16 (e >= -100
-// keeps the smallest value normal, e <= 125 the largest finite), so a product of held values takes the bf16 matrix
-// instructions without another rounding.  What 4 bits cannot hold: an infinity is held as +-6 * 2^125, a NaN as zero; what is
-// read back is always finite.
+// +-{0, 0.5, 1, 1.5, 2, 3, 4, 6} * 2^e, rounded to nearest with ties to the even code: off by at most 2^e, half of the widest gap,
+// where the group's largest value is above 3 * 2^e (or e is -100).  All of it is exact in bfloat16 (e >= -100 keeps the smallest
+// value normal, e <= 125 the largest finite), so a product of held values takes the bf16 matrix instructions without another
+// rounding.  What 4 bits cannot hold: an infinity is held as +-6 * 2^125, a NaN as zero; what is read back is always finite.
 #pragma once
 #include "sp_device.h"
 

@@ -413,8 +413,9 @@ template <int NS, int OUT>
 static void go_few(Fp4GemmArgs& a, hipStream_t st) {
   a.tiles = (a.N / 16 + NS - 1) / NS;
   const dim3 grid(a.tiles * a.S), block(NS <= 2 ? 512 : 256);
-  if (a.frag) hipLaunchKernelGGL((k_fp4_few<NS, OUT, true>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((k_fp4_few<NS, OUT, false>), grid, block, 0, st, a);
+  if constexpr (OUT != OUT_ROWS)                    // (rows of a call of its own are row-major)
+    if (a.frag) { hipLaunchKernelGGL((k_fp4_few<NS, OUT, true>), grid, block, 0, st, a); return; }
+  hipLaunchKernelGGL((k_fp4_few<NS, OUT, false>), grid, block, 0, st, a);
 }
 template <int MT, int NS, int OUT>
 static void go_many(Fp4GemmArgs& a, hipStream_t st) {

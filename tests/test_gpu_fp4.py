@@ -357,6 +357,13 @@ def test_attention_over_long_contexts(heads, P, T):
     attention_case(shape(*heads), [(P, T)])
 
 
+@pytest.mark.parametrize("heads", [(8, 1, 128), (2, 1, 64)])
+@pytest.mark.parametrize("P,T", [(20000, 1), (52000, 3)])
+def test_attention_in_more_chunks_than_a_wave_has_lanes(heads, P, T):
+    """One KV head over a long range: a chunk for most of the CUs."""
+    attention_case(shape(*heads), [(P, T)])
+
+
 @pytest.mark.parametrize("page", [0, 32, 64, 256])
 @pytest.mark.parametrize("heads", [(32, 8, 128), (16, 4, 64)])
 def test_attention_of_ragged_batches(heads, page):
