@@ -92,6 +92,11 @@ def test_products_of_every_cut(m, n, k, gated):
     product_case(m, n, k, gated)
 
 
+@pytest.mark.parametrize("m,n,k,gated", [(1 << 17, 16, 32, False), (40000, 48, 96, True), (1 << 16, 32, 288, False)])
+def test_products_of_very_many_rows(m, n, k, gated):
+    product_case(m, n, k, gated)
+
+
 @pytest.mark.parametrize("m,n", [(1, 4096), (12, 1024), (30, 4096), (64, 4096), (100, 28672), (150, 28672), (200, 28672)])
 def test_columns_past_the_end_count_as_nothing(m, n):
     """Storage goes on to a multiple of 256 columns.  Whatever was in shared memory before: here NaN, out of a product before."""
