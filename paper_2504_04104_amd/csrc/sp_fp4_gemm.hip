@@ -127,20 +127,22 @@ __global__ void __launch_bounds__(NS <= 2 ? 512 : 256) k_fp4_few(Fp4GemmArgs a) 
 // The waves share the rows of X through LDS, which a load brings there without registers, and have NS strips each over all columns
 // of the slice.  A chunk is 128 columns, half a unit; loads are three chunks ahead (five are no faster), a chunk's rows before its
 // weights, and go out between the products: all at once behind the barrier they held up the matrix cores (4096 x 14336, 64 rows,
-// four tiles and four strips whole 91.8 us, 83.3 between).
+// four tiles and four strips whole 91.8 us, 83.3 between).  Up to two tiles, two groups of four waves take a chunk in turn and add
+// their sums through LDS: two waves a SIMD, half the steps (64 rows of 4096 x 4096 10.4 -> 8.6 us); with more tiles that is level.
 #define PANELS 4
 #define AHEAD 3
+constexpr int groups_of(int mt) { return mt <= 2 ? 2 : 1; }
 template <int MT, int NS, int OUT>
-__global__ void __launch_bounds__(256, MT * NS <= 16 ? 2 : 1) k_fp4_many(Fp4GemmArgs a) {
-  constexpr int PANEL = MT * 4096, LOADS = MT + 2 * NS;
+__global__ void __launch_bounds__(256 * groups_of(MT), MT * NS <= 16 ? 2 : 1) k_fp4_many(Fp4GemmArgs a) {
+  constexpr int G = groups_of(MT), PANEL = MT * 4096, LOADS = MT + 2 * NS;
   // arrays of their own, so that the compiler knows which loads a read has to wait for
-  __shared__ __attribute__((aligned(16))) char p0[PANEL];
-  __shared__ __attribute__((aligned(16))) char p1[PANEL];
-  __shared__ __attribute__((aligned(16))) char p2[PANEL];
-  __shared__ __attribute__((aligned(16))) char p3[PANEL];
-#define SP_PAN(i) ((i) == 0 ? p0 : (i) == 1 ? p1 : (i) == 2 ? p2 : p3)
+  __shared__ __attribute__((aligned(16))) char p0[G * PANEL];
+  __shared__ __attribute__((aligned(16))) char p1[G * PANEL];
+  __shared__ __attribute__((aligned(16))) char p2[G * PANEL];
+  __shared__ __attribute__((aligned(16))) char p3[G * PANEL];
+#define SP_PAN(i) (((i) == 0 ? p0 : (i) == 1 ? p1 : (i) == 2 ? p2 : p3) + grp * PANEL)
   auto uni = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
-  const int wave = uni((int)threadIdx.x >> 6), lane = threadIdx.x & 63, l15 = lane & 15, kg = lane >> 4;
+  const int grp = G == 1 ? 0 : uni((int)threadIdx.x >> 8), wave = uni((int)threadIdx.x >> 6) & 3, lane = threadIdx.x & 63, l15 = lane & 15, kg = lane >> 4;
   // the row blocks of a column tile on one XCD, one after the other
   const int id = blockIdx.x, local = id >> 3;
   const int rb = uni(local % a.row_blocks), ts = uni((local / a.row_blocks) * 8 + (id & 7));
@@ -173,6 +175,10 @@ __global__ void __launch_bounds__(256, MT * NS <= 16 ? 2 : 1) k_fp4_many(Fp4Gemm
   int read_at[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) read_at[j] = ((kg >> 1) * 2 + (l15 >> 3)) * 1024 + (l15 & 7) * 128 + (((kg & 1) * 4 + j) ^ (l15 & 7) ^ (l15 >> 3)) * 16;
+  // the groups take a chunk in turn: chunk of step i, and half of the unit it is
+#define SP_C(i) (c_begin + G * (i) + grp)
+#define SP_HALF(I) (G == 1 ? (I) & 1 : grp)
+  const int steps = (c_end - c_begin + G - 1) / G;
   // the word with the lane's two scales, and the turn that brings the first into the exponent field
   const int scale_at = 2048 + (lane & 62) * 2, turn = (lane & 1) * 16 + 9;
   u32x4_t wb[PANELS][NS];
@@ -192,7 +198,7 @@ __global__ void __launch_bounds__(256, MT * NS <= 16 ? 2 : 1) k_fp4_many(Fp4Gemm
 #define SP_LOAD_W(I, C, s)                                                                                             \
   {                                                                                                                    \
     const auto wr_ = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(w[s]), (short)0, (C) < c_end ? live[s] : 0, 0x00020000); \
-    wb[I][s] = __builtin_amdgcn_raw_buffer_load_b128(wr_, lane16 + ((I) & 1) * 1024, ((C) >> 1) * UNIT_BYTES, 0);      \
+    wb[I][s] = __builtin_amdgcn_raw_buffer_load_b128(wr_, lane16 + SP_HALF(I) * 1024, ((C) >> 1) * UNIT_BYTES, 0);      \
     ws[I][s] = __builtin_amdgcn_raw_buffer_load_b32(wr_, scale_at, ((C) >> 1) * UNIT_BYTES, 0);                        \
   }
 #define SP_READ(I, j, Q)                                                                                               \
@@ -204,7 +210,7 @@ __global__ void __launch_bounds__(256, MT * NS <= 16 ? 2 : 1) k_fp4_many(Fp4Gemm
     if ((j) < 3) { SP_READ(I, (j) + 1, ((j) + 1) & 1) } else { SP_READ(((I) + 1) % PANELS, 0, 0) }                     \
     LOADS                                                                                                              \
     _Pragma("unroll") for (int i = 0; i < NS; ++i) {                                                                   \
-      const u32x4_t wf = fp4_to_bf16x8(wb[I][i][j], __uint_as_float(__builtin_amdgcn_alignbit(ws[I][i], ws[I][i], turn + ((I) & 1) * 8))); \
+      const u32x4_t wf = fp4_to_bf16x8(wb[I][i][j], __uint_as_float(__builtin_amdgcn_alignbit(ws[I][i], ws[I][i], turn + SP_HALF(I) * 8))); \
       _Pragma("unroll") for (int t = 0; t < MT; ++t)                                                                   \
           acc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, wf),                        \
                                                               __builtin_bit_cast(bf16x8_t, xq[(j) & 1][t]), acc[t][i], 0, 0, 0); \
@@ -222,8 +228,8 @@ __global__ void __launch_bounds__(256, MT * NS <= 16 ? 2 : 1) k_fp4_many(Fp4Gemm
   {                                                                                                                    \
     SP_WAIT_VMEM((AHEAD - 2) * LOADS + 2 * NS);                                                                        \
     bare_barrier();                                                                                                    \
-    const int ahead_ = (C) + AHEAD;                                                                             \
-    SP_STEP(I, 0, SP_LOAD_X(((I) + AHEAD) % PANELS, ahead_))                                                    \
+    const int ahead_ = SP_C((C) + AHEAD);                                                                              \
+    SP_STEP(I, 0, SP_LOAD_X(((I) + AHEAD) % PANELS, ahead_))                                                           \
     SP_STEP(I, 1, _Pragma("unroll") for (int s = 0; s < NS; s += 2) SP_LOAD_W(((I) + AHEAD) % PANELS, ahead_, s)) \
     SP_STEP(I, 2, _Pragma("unroll") for (int s = 1; s < NS; s += 2) SP_LOAD_W(((I) + AHEAD) % PANELS, ahead_, s)) \
     SP_STEP(I, 3, )                                                                                                    \
@@ -231,29 +237,29 @@ __global__ void __launch_bounds__(256, MT * NS <= 16 ? 2 : 1) k_fp4_many(Fp4Gemm
 #define SP_CHUNK_PRODUCTS(I) { SP_STEP(I, 0, ) SP_STEP(I, 1, ) SP_STEP(I, 2, ) SP_STEP(I, 3, ) }
 #pragma unroll
   for (int p = 0; p < AHEAD; ++p) {
-    SP_LOAD_X(p, c_begin + p)
+    SP_LOAD_X(p, SP_C(p))
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int s = 0; s < NS; ++s) SP_LOAD_W(p, c_begin + p, s)
+    for (int s = 0; s < NS; ++s) SP_LOAD_W(p, SP_C(p), s)
     __builtin_amdgcn_sched_barrier(0);
   }
   SP_WAIT_VMEM((AHEAD - 1) * LOADS + 2 * NS);
   bare_barrier();
   u32x4_t xq[2][MT];
   SP_READ(0, 0, 0)
-  int c = c_begin;
-  for (; c + PANELS <= c_end; c += PANELS) {
+  int c = 0;
+  for (; c + PANELS <= steps; c += PANELS) {
     SP_CHUNK(0, c)
     SP_CHUNK(1, c + 1)
     SP_CHUNK(2, c + 2)
     SP_CHUNK(3, c + 3)
   }
   SP_WAIT_VMEM(0);
-  if (c < c_end) {                                  // up to three are left, and have been asked for
+  if (c < steps) {                                  // up to three are left, and have been asked for
     bare_barrier();
     SP_CHUNK_PRODUCTS(0)
-    if (c + 1 < c_end) SP_CHUNK_PRODUCTS(1)
-    if (c + 2 < c_end) SP_CHUNK_PRODUCTS(2)
+    if (c + 1 < steps) SP_CHUNK_PRODUCTS(1)
+    if (c + 2 < steps) SP_CHUNK_PRODUCTS(2)
   }
 #undef SP_CHUNK_PRODUCTS
 #undef SP_STEP
@@ -262,6 +268,26 @@ __global__ void __launch_bounds__(256, MT * NS <= 16 ? 2 : 1) k_fp4_many(Fp4Gemm
 #undef SP_CHUNK
 #undef SP_READ
 #undef SP_PAN
+#undef SP_C
+#undef SP_HALF
+  if constexpr (G > 1) {
+    // the second group's sums to the first, in the first panel's place
+    static_assert(MT * NS * 4096 <= G * PANEL, "the sums of four waves");
+    f32x4_t* const sums = reinterpret_cast<f32x4_t*>(p0) + wave * MT * NS * 64 + lane;
+    __syncthreads();
+    if (grp) {
+#pragma unroll
+      for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int i = 0; i < NS; ++i) sums[(t * NS + i) * 64] = acc[t][i];
+    }
+    __syncthreads();
+    if (grp) return;
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+      for (int i = 0; i < NS; ++i) acc[t][i] += sums[(t * NS + i) * 64];
+  }
 
   // a lane's four sums: row t * 16 + l15 of X, rows kg * 4 .. + 3 of the strip
 #pragma unroll
@@ -371,25 +397,26 @@ hipError_t sp_launch_fp4_unpack(const void* in, void* out, int N, int K, hipStre
 
 // How a product is cut: tiles of rows (0: the kernel for few rows) and strips of a workgroup, and slices of the columns, whose
 // sums are joined by a launch of their own (`join` us; 0 where whoever takes the partial sums adds them up).  What is least by
-// these times: a chunk of 128 columns, of 112 with at most one workgroup on a CU, 0.25 us for one tile and two strips, 0.28 for
+// these times: a chunk of 128 columns, of 112 with at most one workgroup on a CU, 0.22 us for one tile and two strips, 0.27 for
 // two tiles, 0.40 and 0.66 for four with two and four strips, 0.82 for five, 1.12 for seven; a unit of a wave of the kernel for
-// few rows 1 us and more with every row; a megabyte of partial sums 0.3.  Workgroups past the CUs take turns: two at a time on a
-// CU are not faster than one after the other.  Us a call, as chosen and next to it (tiles x strips): 28672 x 4096 gated, 64 rows
-// 4 x 2 20.4 (2 x 2 23.9, 4 x 4 27.4), 100 rows 4 x 4 29.3 (4 x 2 30.9), 160 rows 5 x 4 36.7 (4 x 4 45.2), 200 rows 7 x 4 46.4
-// (4 x 4 47.9), 256 rows 4 x 4 51.7 (7 x 4 84.2); 4096 x 14336, 17 rows 2 x 2 in 8 slices 13.2 (in 4 15.2, whole 35.8), 64 rows
-// in 4 16.2 (in 8 18.0), 200 rows 4 x 4 in 4 31.9 (2 x 2 whole 37.5); with the kernel for few rows, 4096 x 4096, one row 7.5 (one
-// tile whole 10.1, in 4 slices 11.8), 16 rows 8.5 (10.4); 4096 x 14336, one row 11.7 (one tile in 8 slices 12.0), nine 14.8 (12.6);
-// 28672 x 4096 gated, one row with one tile 14.6 (few rows' 15.9), 16 rows 15.0 (19.9).
+// few rows 1 us and more with every row, and 0.8 more before them; a megabyte of partial sums 0.3.  Workgroups past the CUs take
+// turns: two at a time on a CU are not faster than one after the other.  Us a call, as chosen and next to it (tiles x strips):
+// 28672 x 4096 gated, 64 rows 4 x 2 20.4 (2 x 2 23.9, 4 x 4 27.4), 100 rows 4 x 4 28.4 (4 x 2 30.9), 160 rows 5 x 4 35.2 (4 x 4
+// 45.2), 200 rows 7 x 4 45.4 (4 x 4 47.9), 256 rows 4 x 4 49.9 (7 x 4 84.2); 4096 x 14336, 17 rows 2 x 2 in 8 slices 13.2 (in 4
+// 15.2, whole 35.8), 64 rows in 4 16.2 (in 8 18.0), 200 rows 4 x 4 in 4 31.9 (2 x 2 whole 37.5); 4096 x 4096, one row with the kernel
+// for few rows 7.4 (one tile 8.3, in 4 slices 11.6), 64 rows one tile 8.6 (two 10.2, in 4 slices 11.6), 200 rows two tiles 11.0 (one
+// 13.3); 4096 x 14336, one row with the kernel for few rows 11.6 (one tile in 8 slices 12.4), nine rows with one tile 12.7 (few rows'
+// 14.8); 28672 x 4096 gated, one row with one tile 14.6 (few rows' 15.9), 16 rows 14.7 (19.9).
 struct Fp4Split { int mt, ns, S; };
 static Fp4Split split_of(int M, int N, int K, int n_cu, float join, int most_slices) {
-  static const struct { int mt, ns; float us; } tiled[] = {{1, 2, .25f}, {2, 2, .28f}, {4, 2, .40f}, {4, 4, .66f}, {5, 4, .82f}, {7, 4, 1.12f}};
-  static const struct { int ns, waves; float us, us_row; } few[] = {{1, 8, 1.f, .07f}, {2, 8, 1.6f, .06f}, {4, 4, 1.f, .06f}};
+  static const struct { int mt, ns; float us; } tiled[] = {{1, 2, .22f}, {2, 2, .27f}, {4, 2, .40f}, {4, 4, .66f}, {5, 4, .82f}, {7, 4, 1.12f}};
+  static const struct { int ns, waves; float us, us_row; } few[] = {{1, 8, 1.f, .07f}, {2, 8, 1.6f, .10f}, {4, 4, 1.f, .06f}};
   const int units = (K + UNIT_K - 1) / UNIT_K, strips = N / 16;
   Fp4Split best = {0, 1, 1};
   float least = 1e30f;
   if (M <= 16 && sp_fp4_bytes(N, K) < 1u << 31)     // (few rows: gate and up rows in one buffer)
     for (const auto& f : few) {
-      const float us = (float)(((strips + f.ns - 1) / f.ns + n_cu - 1) / n_cu) * ((units + f.waves - 1) / f.waves) * (f.us + f.us_row * M);
+      const float us = .8f + (float)(((strips + f.ns - 1) / f.ns + n_cu - 1) / n_cu) * ((units + f.waves - 1) / f.waves) * (f.us + f.us_row * M);
       if (us < least) { least = us; best = {0, f.ns, 1}; }
     }
   for (const auto& t : tiled) {
@@ -402,7 +429,7 @@ static Fp4Split split_of(int M, int N, int K, int n_cu, float join, int most_sli
   }
   return best;
 }
-#define JOIN_US 6.f
+#define JOIN_US 7.f
 #define MOST_SLICES 16
 size_t sp_fp4_product_floats(int M, int N, int K, int n_cu) {
   const Fp4Split f = split_of(M, N, K, n_cu, JOIN_US, MOST_SLICES);
@@ -422,7 +449,7 @@ static void go_many(Fp4GemmArgs& a, hipStream_t st) {
   const int strips = OUT == OUT_GATED ? a.N / 32 : a.N / 16, per = OUT == OUT_GATED ? 2 * NS : 4 * NS;
   a.row_blocks = (a.M + 16 * MT - 1) / (16 * MT);
   a.tiles = (strips + per - 1) / per;
-  hipLaunchKernelGGL((k_fp4_many<MT, NS, OUT>), dim3((a.tiles * a.S + 7) / 8 * 8 * a.row_blocks), dim3(256), 0, st, a);
+  hipLaunchKernelGGL((k_fp4_many<MT, NS, OUT>), dim3((a.tiles * a.S + 7) / 8 * 8 * a.row_blocks), dim3(256 * groups_of(MT)), 0, st, a);
 }
 template <int OUT>
 static hipError_t launch(const Fp4Split& f, Fp4GemmArgs& a, hipStream_t st) {
