@@ -317,6 +317,10 @@ __device__ __forceinline__ void attn_fp4(const Fp4AttnArgs& a, const AttnPlan& p
       for (int c = 0; c < CW; ++c) o[c] *= alpha;
       shift = lower;
     }
+    // The weights are rounded to bf16 here, as those over a bf16 cache are, and their sum is that of the rounded ones: each is off
+    // by half a step, 2^-8 of itself, at most.  Results are 0.213-0.231 % from 64-bit ones (root mean squares, normal inputs), of
+    // which 0.166 is their own rounding to bf16.  Weights as two bf16 numbers each leave those 0.166, but take every product below
+    // twice: 64 rows behind 2048 slots 11.6 -> 12.6 us, 32 requests of 1-8 rows 21.9 -> 25.3, 128 rows of 64 heads 27.6 -> 32.1.
     u32x4_t pb;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
