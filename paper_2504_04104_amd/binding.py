@@ -196,6 +196,13 @@ def _at(a) -> int:
     return a.buffer_info()[0]
 
 
+def _matrix_shape(shape, name: str):
+    """(rows, columns) of a layer's projection matrix."""
+    return {"wqkv": ((shape.n_q_heads + 2 * shape.n_kv_heads) * shape.d_head, shape.d_model),
+            "wo": (shape.d_model, shape.n_q_heads * shape.d_head), "wgu": (2 * shape.d_ff, shape.d_model),
+            "wd": (shape.d_model, shape.d_ff)}[name]
+
+
 def _check(rc: int, what: str):
     if rc != 0:
         raise SpError(rc, what)
@@ -232,8 +239,7 @@ class Stage:
             for name in ("wqkv", "wo", "wgu", "wd", "norm1", "norm2"):
                 t = w[name]
                 if flags & SP_FLAG_FP4_WEIGHTS and not name.startswith("norm"):
-                    rows, cols = self._matrix_shape(name)
-                    assert isinstance(t, Fp4Matrix) and (t.n_rows, t.n_cols) == (rows, cols), name
+                    assert isinstance(t, Fp4Matrix) and (t.n_rows, t.n_cols) == _matrix_shape(shape, name), name
                     t = t.data
                     assert t.is_cuda and t.is_contiguous(), name
                 else:
@@ -266,11 +272,6 @@ class Stage:
             self.close()
         except Exception:
             pass
-
-    def _matrix_shape(self, name: str):
-        s = self.shape
-        return {"wqkv": ((s.n_q_heads + 2 * s.n_kv_heads) * s.d_head, s.d_model), "wo": (s.d_model, s.n_q_heads * s.d_head),
-                "wgu": (2 * s.d_ff, s.d_model), "wd": (s.d_model, s.d_ff)}[name]
 
     def kv_view(self):
         """The slab as a tensor [layer, K|V, kv_head, slot, d_head] (no copy)."""
@@ -693,8 +694,10 @@ def fp4_pack_weights(shape, layers: List[Dict[str, "object"]]):
         o = dict(w)
         a, b = sp_layer_weights(), sp_layer_weights()
         for name in ("wqkv", "wo", "wgu", "wd"):
+            # (the call reads and writes the sizes of `shape`)
             assert w[name].is_cuda and w[name].is_contiguous() and w[name].dtype == torch.bfloat16, name
-            o[name] = _fp4_empty(int(w[name].shape[0]), int(w[name].shape[1]), w[name].device)
+            assert tuple(w[name].shape) == _matrix_shape(shape, name) and w[name].device == w["wqkv"].device, name
+            o[name] = _fp4_empty(*_matrix_shape(shape, name), w[name].device)
             setattr(a, name, w[name].data_ptr())
             setattr(b, name, o[name].data.data_ptr())
         device = w["wqkv"].device

@@ -1,0 +1,62 @@
+"""What the binding of the 4-bit entry points checks before anything reaches a device."""
+import contextlib
+
+import pytest
+import torch
+
+import paper_2504_04104_amd as sp
+import workloads as wl
+from paper_2504_04104_amd import binding
+
+SHAPE = wl.ModelShape(1, 256, 4, 2, 128, 512, 1e-5, 500000.0, "bf16")
+SIZES = {"wqkv": (1024, 256), "wo": (256, 512), "wgu": (1024, 256), "wd": (256, 512)}
+
+
+class OnDevice:
+    """A host tensor that says it is on a device."""
+    is_cuda = True
+
+    def __init__(self, t):
+        self.t = t
+
+    def __getattr__(self, name):
+        return getattr(self.t, name)
+
+
+def layer(**other):
+    return {n: OnDevice(torch.zeros(other.get(n, s), dtype=torch.bfloat16)) for n, s in SIZES.items()}
+
+
+@pytest.fixture
+def packed(monkeypatch):
+    """The calls of sp_fp4_pack_weights that would have been made."""
+    lib, calls = sp.load_library(), []
+
+    class Library:
+        sp_fp4_matrix_bytes = lib.sp_fp4_matrix_bytes
+
+        def sp_fp4_pack_weights(self, *args):
+            calls.append(args)
+            return 0
+    monkeypatch.setattr(binding, "load_library", lambda: Library())
+    monkeypatch.setattr(binding, "_raw_stream", lambda device: None)
+    monkeypatch.setattr(torch.cuda, "device", lambda device: contextlib.nullcontext())
+    return calls
+
+
+@pytest.mark.parametrize("name", sorted(SIZES))
+def test_weights_of_another_shape_than_the_models_are_not_packed(packed, name):
+    rows, cols = SIZES[name]
+    for size in ((rows - 16, cols), (rows + 16, cols), (rows, cols // 2), (cols, rows), (1, rows, cols), (rows * cols,)):
+        if size == (rows, cols):
+            continue
+        with pytest.raises(AssertionError):
+            sp.fp4_pack_weights(SHAPE, [layer(**{name: size})])
+    assert not packed
+
+
+def test_weights_of_the_models_shape_are_packed(packed):
+    out = sp.fp4_pack_weights(SHAPE, [layer()])[0]
+    assert len(packed) == 1
+    for name, (rows, cols) in SIZES.items():
+        assert (out[name].n_rows, out[name].n_cols) == (rows, cols) and out[name].data.numel() == rows * ((cols + 255) // 256) * 136
