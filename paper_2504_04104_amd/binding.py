@@ -642,9 +642,15 @@ def pack_matrix(w, device: str = "cuda:0"):
 
 # ---- 4-bit weights ------------------------------------------------------------------------
 class Fp4Matrix:
-    """A matrix of 4-bit weights: the packed bytes (a uint8 device tensor) and its shape."""
+    """A matrix of 4-bit weights: the packed bytes (a uint8 device tensor of sp_fp4_matrix_bytes) and its shape."""
 
     def __init__(self, data, n_rows: int, n_cols: int):
+        import torch
+        size = load_library().sp_fp4_matrix_bytes(n_rows, n_cols)
+        if size == 0:
+            raise SpError(-9, "a %d x %d matrix in 4 bits" % (n_rows, n_cols))
+        # (the calls read as many bytes as the shape says)
+        assert data.dtype == torch.uint8 and data.is_contiguous() and data.numel() == size
         self.data, self.n_rows, self.n_cols = data, n_rows, n_cols
 
 
@@ -656,8 +662,6 @@ def _raw_stream(device):
 def _fp4_empty(n_rows: int, n_cols: int, device) -> Fp4Matrix:
     import torch
     size = load_library().sp_fp4_matrix_bytes(n_rows, n_cols)
-    if size == 0:
-        raise SpError(-9, "a %d x %d matrix in 4 bits" % (n_rows, n_cols))
     return Fp4Matrix(torch.empty(size, dtype=torch.uint8, device=device), n_rows, n_cols)
 
 

@@ -60,3 +60,16 @@ def test_weights_of_the_models_shape_are_packed(packed):
     assert len(packed) == 1
     for name, (rows, cols) in SIZES.items():
         assert (out[name].n_rows, out[name].n_cols) == (rows, cols) and out[name].data.numel() == rows * ((cols + 255) // 256) * 136
+
+
+def test_a_matrix_holds_as_many_bytes_as_its_shape_takes():
+    size = 3 * 2 * 2176                             # 48 x 288: strips of 16 rows, two units of 256 columns
+    assert sp.Fp4Matrix(torch.zeros(size, dtype=torch.uint8), 48, 288).n_cols == 288
+    for data in (torch.zeros(size - 1, dtype=torch.uint8), torch.zeros(size + 2176, dtype=torch.uint8), torch.zeros(size, dtype=torch.int8),
+                 torch.zeros(2 * size, dtype=torch.uint8)[::2], torch.zeros(0, dtype=torch.uint8)):
+        with pytest.raises(AssertionError):
+            sp.Fp4Matrix(data, 48, 288)
+    for rows, cols in ((17, 32), (0, 32), (16, 40), (1 << 18, 32)):
+        with pytest.raises(sp.SpError) as err:
+            sp.Fp4Matrix(torch.zeros(size, dtype=torch.uint8), rows, cols)
+        assert err.value.status == -9
