@@ -184,16 +184,22 @@ def _f32(a: Optional[Sequence[float]]):
 
 
 def _ids(a: Sequence[int]):
-    """Plain integers as an array that ctypes takes by its address (`_at`); what array() does not take is numpy's to cast or
-    refuse, as in _i32."""
-    try:
-        return array.array("i", a)
-    except (TypeError, OverflowError):
-        return array.array("i", np.ascontiguousarray(np.asarray(a, dtype=np.int32)).tobytes())
+    """Integers as an array that ctypes takes by its address (`_at`): lists the short way; everything else, and what array() does
+    not take, is numpy's to cast or refuse, as in _i32."""
+    if type(a) is list:
+        try:
+            return array.array("i", a)
+        except (TypeError, OverflowError):
+            pass
+    return array.array("i", np.ascontiguousarray(np.asarray(a, dtype=np.int32)).tobytes())
+
+
+_NOTHING = array.array("i", [0])
 
 
 def _at(a) -> int:
-    return a.buffer_info()[0]
+    # (an empty array has no address, and a call without requests is a call)
+    return a.buffer_info()[0] or _NOTHING.buffer_info()[0]
 
 
 def _matrix_shape(shape, name: str):

@@ -1,6 +1,8 @@
 """What the binding of the 4-bit entry points checks before anything reaches a device."""
 import contextlib
+import ctypes as C
 
+import numpy as np
 import pytest
 import torch
 
@@ -73,3 +75,23 @@ def test_a_matrix_holds_as_many_bytes_as_its_shape_takes():
         with pytest.raises(sp.SpError) as err:
             sp.Fp4Matrix(torch.zeros(size, dtype=torch.uint8), rows, cols)
         assert err.value.status == -9
+
+
+def test_a_call_without_requests_has_arrays_too():
+    for empty in ([], (), np.zeros(0, np.int64)):
+        a = binding._ids(empty)
+        assert len(a) == 0 and binding._at(a) != 0
+
+
+def test_host_arrays_are_cast_and_refused_as_those_of_the_forward_call():
+    for given in ([3, 0, -1], (3, 0, -1), np.array([3, 0, -1], np.int64), [np.int64(3), False, -1], [3.0, 0.0, -1.0], torch.tensor([3, 0, -1]), range(3, 0, -1)):
+        a, want = binding._ids(given), binding._i32(given)[0]
+        assert list(a) == list(want)
+        assert C.cast(binding._at(a), C.POINTER(C.c_int32))[:len(a)] == list(a)
+    for refused in (b"\x00\x00\x00\x00", "ab", [None], [1 << 40], object()):
+        errors = []
+        for way in (binding._i32, binding._ids):
+            with pytest.raises(Exception) as err:
+                way(refused)
+            errors.append(err.type)
+        assert errors[0] is errors[1], refused
