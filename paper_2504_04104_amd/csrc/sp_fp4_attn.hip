@@ -332,6 +332,10 @@ __device__ __forceinline__ void attn_fp4(const Fp4AttnArgs& a, const AttnPlan& p
       o[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, vf[c]), __builtin_bit_cast(bf16x8_t, pb), o[c], 0, 0, 0);
   }
 
+  // The loop has asked for a tile that nobody reads: its scales have to be in LDS before the workgroup gives that away.  (Its ten
+  // loads of codes came after them, and go to registers.)
+  SP_WAIT_VMEM(10);
+
   // ---- fold the waves' states (fixed order, so results do not depend on timing) ----
   // (the lane's number is asked for again: carried through the loop, it and what comes of it cost registers)
   const int again = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)), row = again & 15, part = again >> 4;
