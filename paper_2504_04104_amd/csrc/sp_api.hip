@@ -9,6 +9,7 @@
 #include <vector>
 
 #include "../../include/specpipe.h"
+#include "sp_known.h"
 #include "sp_launch.h"
 
 static_assert(SP_T == SP_MAX_TREE_NODES, "tree capacity");
@@ -446,13 +447,15 @@ static bool fp4_shape(int64_t n_rows, int64_t n_cols) {
   return n_rows >= 16 && n_cols >= 32 && n_rows % 16 == 0 && n_cols % 32 == 0 && n_rows <= SP_FP4_MAX_DIM && n_cols <= SP_FP4_MAX_DIM;
 }
 // compute units of the current device
+static KnownNumbers<SP_NOALLOC_MAX_DEVICES> g_cus;
 static int current_cus() {
-  static int known[SP_NOALLOC_MAX_DEVICES];
-  int dev = 0, cus = 0;
+  int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= SP_NOALLOC_MAX_DEVICES) return 256;
-  if (known[dev] > 0) return known[dev];
-  if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus < 1) return 256;
-  return known[dev] = cus;
+  const int cus = g_cus.of(dev, [dev] {
+    int n = 0;
+    return hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess ? n : 0;
+  });
+  return cus > 0 ? cus : 256;
 }
 
 size_t sp_fp4_matrix_bytes(int32_t n_rows, int32_t n_cols) { return fp4_shape(n_rows, n_cols) ? sp_fp4_bytes(n_rows, n_cols) : 0; }
