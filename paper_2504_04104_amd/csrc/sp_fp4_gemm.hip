@@ -13,9 +13,7 @@
 // L2 and LDS into the matrix cores (64 rows of 28672 x 4096 20.4 us; 200 rows of 57344 x 8192 170 us, 1.1 PFLOP/s).
 #include "sp_launch.h"
 #include "sp_fp4.h"
-
-#define UNIT_K 256
-#define UNIT_BYTES 2176
+#include "sp_fp4_split.h"
 
 enum { OUT_PARTS, OUT_ROWS, OUT_GATED };
 
@@ -383,7 +381,7 @@ __global__ void __launch_bounds__(64) k_fp4_unpack(const char* in, bf16_t* out, 
 }
 
 // ---- launchers -------------------------------------------------------------------
-size_t sp_fp4_bytes(int N, int K) { return (size_t)(N / 16) * ((K + UNIT_K - 1) / UNIT_K) * UNIT_BYTES; }
+size_t sp_fp4_bytes(int N, int K) { return fp4_bytes(N, K); }
 hipError_t sp_launch_fp4_pack(const void* in, void* out, int N, int K, hipStream_t st) {
   const int units = (K + UNIT_K - 1) / UNIT_K;
   hipLaunchKernelGGL(k_fp4_pack, dim3(N / 16 * units), dim3(64), 0, st, (const bf16_t*)in, (char*)out, K, units);
@@ -395,44 +393,8 @@ hipError_t sp_launch_fp4_unpack(const void* in, void* out, int N, int K, hipStre
   return hipGetLastError();
 }
 
-// How a product is cut: tiles of rows (0: the kernel for few rows) and strips of a workgroup, and slices of the columns, whose
-// sums are joined by a launch of their own (`join` us; 0 where whoever takes the partial sums adds them up).  What is least by
-// these times: a chunk of 128 columns, of 112 with at most one workgroup on a CU, 0.22 us for one tile and two strips, 0.27 for
-// two tiles, 0.40 and 0.66 for four with two and four strips, 0.82 for five, 1.12 for seven; a unit of a wave of the kernel for
-// few rows 1 us and more with every row, and 0.8 more before them; a megabyte of partial sums 0.3.  Workgroups past the CUs take
-// turns: two at a time on a CU are not faster than one after the other.  Us a call, as chosen and next to it (tiles x strips):
-// 28672 x 4096 gated, 64 rows 4 x 2 20.4 (2 x 2 23.9, 4 x 4 27.4), 100 rows 4 x 4 28.4 (4 x 2 30.9), 160 rows 5 x 4 35.2 (4 x 4
-// 45.2), 200 rows 7 x 4 45.4 (4 x 4 47.9), 256 rows 4 x 4 49.9 (7 x 4 84.2); 4096 x 14336, 17 rows 2 x 2 in 8 slices 13.2 (in 4
-// 15.2, whole 35.8), 64 rows in 4 16.2 (in 8 18.0), 200 rows 4 x 4 in 4 31.9 (2 x 2 whole 37.5); 4096 x 4096, one row with the kernel
-// for few rows 7.4 (one tile 8.3, in 4 slices 11.6), 64 rows one tile 8.6 (two 10.2, in 4 slices 11.6), 200 rows two tiles 11.0 (one
-// 13.3); 4096 x 14336, one row with the kernel for few rows 11.6 (one tile in 8 slices 12.4), nine rows with one tile 12.7 (few rows'
-// 14.8); 28672 x 4096 gated, one row with one tile 14.6 (few rows' 15.9), 16 rows 14.7 (19.9).
-struct Fp4Split { int mt, ns, S; };
-static Fp4Split split_of(int M, int N, int K, int n_cu, float join, int most_slices) {
-  static const struct { int mt, ns; float us; } tiled[] = {{1, 2, .22f}, {2, 2, .27f}, {4, 2, .40f}, {4, 4, .66f}, {5, 4, .82f}, {7, 4, 1.12f}};
-  static const struct { int ns, waves; float us, us_row; } few[] = {{1, 8, 1.f, .07f}, {2, 8, 1.6f, .10f}, {4, 4, 1.f, .06f}};
-  const int units = (K + UNIT_K - 1) / UNIT_K, strips = N / 16;
-  Fp4Split best = {0, 1, 1};
-  float least = 1e30f;
-  if (M <= 16 && sp_fp4_bytes(N, K) < 1u << 31)     // (few rows: gate and up rows in one buffer)
-    for (const auto& f : few) {
-      const float us = .8f + (float)(((strips + f.ns - 1) / f.ns + n_cu - 1) / n_cu) * ((units + f.waves - 1) / f.waves) * (f.us + f.us_row * M);
-      if (us < least) { least = us; best = {0, f.ns, 1}; }
-    }
-  for (const auto& t : tiled) {
-    const long long wgs = (long long)((strips + 4 * t.ns - 1) / (4 * t.ns)) * ((M + 16 * t.mt - 1) / (16 * t.mt));
-    for (int S = 1; S <= most_slices && S <= units; ++S) {
-      if (S > 1 && wgs * S > 2 * n_cu) break;
-      const float us = (float)((wgs * S + n_cu - 1) / n_cu) * ((units + S - 1) / S * 2) * t.us + (S > 1 ? join + (float)S * M * N * 1.2e-6f : 0.f);
-      if (us < least) { least = us; best = {t.mt, t.ns, S}; }
-    }
-  }
-  return best;
-}
-#define JOIN_US 7.f
-#define MOST_SLICES 16
 size_t sp_fp4_product_floats(int M, int N, int K, int n_cu) {
-  const Fp4Split f = split_of(M, N, K, n_cu, JOIN_US, MOST_SLICES);
+  const Fp4Split f = fp4_split_call(M, N, K, n_cu);
   return f.S > 1 ? (size_t)f.S * M * N : 0;
 }
 
@@ -470,21 +432,20 @@ static hipError_t launch(const Fp4Split& f, Fp4GemmArgs& a, hipStream_t st) {
 
 hipError_t sp_launch_fp4_parts(const bf16_t* X, bool frag, const void* W, float* out, int M, int N, int K, int n_cu, size_t part_floats,
                                int* S_out, hipStream_t st) {
-  Fp4Split f = split_of(M, N, K, n_cu, 0.f, MOST_SLICES);
-  while (f.S > 1 && (size_t)f.S * M * N > part_floats) --f.S;
-  if ((size_t)f.S * M * N > part_floats) return hipErrorInvalidValue;
+  const Fp4Split f = fp4_split_parts(M, N, K, n_cu, part_floats);
+  if (f.S < 1) return hipErrorInvalidValue;
   *S_out = f.S;
   Fp4GemmArgs a{X, (const char*)W, out, M, N, K, (K + UNIT_K - 1) / UNIT_K, f.S, 0, 0, frag, false};
   return launch<OUT_PARTS>(f, a, st);
 }
 hipError_t sp_launch_fp4_gateup(const bf16_t* X, bool frag, const void* W, bf16_t* act, int M, int F, int K, int n_cu, hipStream_t st) {
-  const Fp4Split f = split_of(M, 2 * F, K, n_cu, 0.f, 1);
+  const Fp4Split f = fp4_split_gateup(M, F, K, n_cu);
   Fp4GemmArgs a{X, (const char*)W, act, M, 2 * F, K, (K + UNIT_K - 1) / UNIT_K, 1, 0, 0, frag, frag};
   return launch<OUT_GATED>(f, a, st);
 }
 hipError_t sp_launch_fp4_product(const bf16_t* X, const void* W, bool gated, bf16_t* out, float* work, int M, int N, int K, int n_cu,
                                  hipStream_t st) {
-  const Fp4Split f = split_of(M, N, K, n_cu, JOIN_US, MOST_SLICES);
+  const Fp4Split f = fp4_split_call(M, N, K, n_cu);
   Fp4GemmArgs a{X, (const char*)W, out, M, N, K, (K + UNIT_K - 1) / UNIT_K, f.S, 0, 0, false, false};
   if (f.S == 1) return gated ? launch<OUT_GATED>(f, a, st) : launch<OUT_ROWS>(f, a, st);
   a.out = work;

@@ -1,0 +1,97 @@
+"""How products with 4-bit weights are cut (csrc/sp_fp4_split.h, plain C++), and that the GPU tests' cases reach every kernel."""
+import ctypes as C
+import os
+import subprocess
+
+import numpy as np
+import pytest
+
+import paper_2504_04104_amd as sp
+from fp4_cases import FORWARDS, PRODUCTS
+
+DRIVER = r"""
+#include "sp_fp4_split.h"
+extern "C" void cut(int kind, int m, int n, int k, int n_cu, long room, int* o) {
+  const Fp4Split f = kind == 0 ? fp4_split_call(m, n, k, n_cu) : kind == 1 ? fp4_split_parts(m, n, k, n_cu, (size_t)room)
+                                                                           : fp4_split_gateup(m, n, k, n_cu);
+  o[0] = f.mt; o[1] = f.ns; o[2] = f.S;
+}
+extern "C" long bytes(int n, int k) { return (long)fp4_bytes(n, k); }
+"""
+CALL, PARTS, GATEUP = 0, 1, 2
+TILED = [(1, 2), (2, 2), (4, 2), (4, 4), (5, 4), (7, 4)]
+FEW = [(0, 1), (0, 2), (0, 4)]
+
+
+@pytest.fixture(scope="module")
+def lib(tmp_path_factory):
+    d = tmp_path_factory.mktemp("split4")
+    (d / "driver.cpp").write_text(DRIVER)
+    csrc = os.path.join(os.path.dirname(os.path.abspath(__file__)), "..", "paper_2504_04104_amd", "csrc")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-I", csrc, str(d / "driver.cpp"), "-o", str(d / "driver.so")], check=True)
+    out = C.CDLL(str(d / "driver.so"))
+    out.bytes.restype = C.c_long
+    return out
+
+
+def cut(lib, kind, m, n, k, n_cu=256, room=1 << 40):
+    o = (C.c_int * 3)()
+    lib.cut(kind, m, n, k, n_cu, C.c_long(room), o)
+    return tuple(o)
+
+
+def steps(k, S, mt):
+    """Steps of the loop over the chunks of 128 columns, of the longest slice: in turns of four, the rest behind the loop."""
+    units, groups = -(-k // 256), 2 if mt <= 2 else 1
+    return max(-(-(min((s + 1) * units // S * 2, -(-k // 128)) - s * units // S * 2) // groups) for s in range(S))
+
+
+def turns(k, S, mt):
+    """More than two turns of the loop and steps behind it: what a short product, or one that ends with a turn, leaves out."""
+    return steps(k, S, mt) >= 9 and steps(k, S, mt) % 4 != 0
+
+
+def test_cuts_are_within_their_bounds(lib):
+    rng = np.random.default_rng(2)
+    for _ in range(4000):
+        m, n, k = (int(2 ** rng.uniform(0, 17)), 16 * int(2 ** rng.uniform(0, 13)), 32 * int(2 ** rng.uniform(0, 12)))
+        n_cu, room = int(rng.choice([32, 64, 128, 256])), int(2 ** rng.uniform(10, 34))
+        assert lib.bytes(n, k) == sp.load_library().sp_fp4_matrix_bytes(n, k)
+        for kind in (CALL, PARTS, GATEUP):
+            mt, ns, S = cut(lib, kind, m, n if kind != GATEUP else max(16, n // 2), k, n_cu, room)
+            assert (mt, ns) in TILED + FEW
+            assert mt > 0 or (m <= 16 and S <= 1)
+            assert S <= 16 and S <= -(-k // 256) and (kind != GATEUP or S == 1)
+            assert S >= (0 if kind == PARTS else 1) and (kind != PARTS or S * m * n <= room)
+            assert kind != PARTS or S >= 1 or m * n > room
+
+
+def test_products_reach_every_kernel_and_its_loop(lib):
+    seen = set()
+    for m, n, k, gated in PRODUCTS:
+        assert k % 32 == 0 and n % 16 == 0
+        mt, ns, S = cut(lib, CALL, m, n * 2 if gated else n, k)
+        if mt == 0 or turns(k, S, mt):
+            seen.add((mt, ns, S > 1, gated))
+    want = {(mt, ns, cut_, gated) for mt, ns in TILED for cut_ in (False, True) for gated in (False, True)}
+    want |= {(mt, ns, False, gated) for mt, ns in FEW for gated in (False, True)}
+    assert seen == want
+
+
+def forward_cuts(lib, d, nq, nkv, ff, m):
+    """(what, tiles, strips, rows in fragment order, loop) of the four products of a layer."""
+    dq, nqkv, rows = nq * 128, (nq + 2 * nkv) * 128, -(-m // 16) * 16
+    room = max(max(rows, 1024) * max(nqkv, d), rows * 2 * ff)
+    for what, n, k in (("parts", nqkv, d), ("parts", d, dq), ("parts", d, ff), ("gated", ff, d)):
+        mt, ns, S = cut(lib, PARTS if what == "parts" else GATEUP, m, n, k, room=room)
+        yield what, mt, ns, m > 8, mt == 0 or turns(k, S, mt)
+
+
+def test_forward_calls_reach_every_kernel_and_its_loop(lib):
+    seen = set()
+    for case in FORWARDS:
+        seen |= set(forward_cuts(lib, *case))
+    want = {("gated", mt, ns, m > 8, True) for mt, ns in FEW for m in (8, 9)} | {(what, 1, 2, False, True) for what in ("parts", "gated")}
+    want |= {(what, mt, ns, True, True) for mt, ns in TILED for what in ("parts", "gated")}
+    want.add(("parts", 0, 4, False, True))          # one or two rows of more than 32768 columns
+    assert want <= seen
