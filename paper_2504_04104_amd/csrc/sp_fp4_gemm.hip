@@ -402,7 +402,7 @@ template <int NS, int OUT>
 static void go_few(Fp4GemmArgs& a, hipStream_t st) {
   a.tiles = (a.N / 16 + NS - 1) / NS;
   const dim3 grid(a.tiles * a.S), block(NS <= 2 ? 512 : 256);
-  if constexpr (OUT != OUT_ROWS)                    // (rows of a call of its own are row-major)
+  if constexpr (OUT == OUT_GATED)                   // (else row-major: rows of a call of its own, or one or two of a forward call)
     if (a.frag) { hipLaunchKernelGGL((k_fp4_few<NS, OUT, true>), grid, block, 0, st, a); return; }
   hipLaunchKernelGGL((k_fp4_few<NS, OUT, false>), grid, block, 0, st, a);
 }
@@ -416,9 +416,9 @@ static void go_many(Fp4GemmArgs& a, hipStream_t st) {
 template <int OUT>
 static hipError_t launch(const Fp4Split& f, Fp4GemmArgs& a, hipStream_t st) {
   switch (f.mt * 8 + f.ns) {
-    case 1: go_few<1, OUT>(a, st); break;
-    case 2: go_few<2, OUT>(a, st); break;
-    case 4: go_few<4, OUT>(a, st); break;
+    case 1: if constexpr (OUT != OUT_PARTS) { go_few<1, OUT>(a, st); break; } else return hipErrorInvalidValue;
+    case 2: if constexpr (OUT != OUT_PARTS) { go_few<2, OUT>(a, st); break; } else return hipErrorInvalidValue;
+    case 4: if (OUT != OUT_GATED && a.frag) return hipErrorInvalidValue; go_few<4, OUT>(a, st); break;
     case 1 * 8 + 2: go_many<1, 2, OUT>(a, st); break;
     case 2 * 8 + 2: go_many<2, 2, OUT>(a, st); break;
     case 4 * 8 + 2: go_many<4, 2, OUT>(a, st); break;

@@ -19,15 +19,17 @@ inline size_t fp4_bytes(int N, int K) { return (size_t)(N / 16) * ((K + UNIT_K -
 // for few rows 7.4 (one tile 8.3, in 4 slices 11.6), 64 rows one tile 8.6 (two 10.2, in 4 slices 11.6), 200 rows two tiles 11.0 (one
 // 13.3); 4096 x 14336, one row with the kernel for few rows 11.6 (one tile in 8 slices 12.4), nine rows with one tile 12.7 (few rows'
 // 14.8); 28672 x 4096 gated, one row with one tile 14.6 (few rows' 15.9), 16 rows 14.7 (19.9).  Three and six tiles have no kernel.
+// The kernel for few rows is for up to `few_rows` of them and takes `few_strips` at least.
 struct Fp4Split { int mt, ns, S; };
-inline Fp4Split fp4_split(int M, int N, int K, int n_cu, float join, int most_slices) {
+inline Fp4Split fp4_split(int M, int N, int K, int n_cu, float join, int most_slices, int few_rows = 16, int few_strips = 1) {
   static const struct { int mt, ns; float us; } tiled[] = {{1, 2, .22f}, {2, 2, .27f}, {4, 2, .40f}, {4, 4, .66f}, {5, 4, .82f}, {7, 4, 1.12f}};
   static const struct { int ns, waves; float us, us_row; } few[] = {{1, 8, 1.f, .07f}, {2, 8, 1.6f, .10f}, {4, 4, 1.f, .06f}};
   const int units = (K + UNIT_K - 1) / UNIT_K, strips = N / 16;
   Fp4Split best = {0, 1, 1};
   float least = 1e30f;
-  if (M <= 16 && fp4_bytes(N, K) < 1u << 31)        // (few rows: gate and up rows in one buffer)
+  if (M <= few_rows && fp4_bytes(N, K) < 1u << 31)  // (few rows: gate and up rows in one buffer)
     for (const auto& f : few) {
+      if (f.ns < few_strips) continue;
       const float us = .8f + (float)(((strips + f.ns - 1) / f.ns + n_cu - 1) / n_cu) * ((units + f.waves - 1) / f.waves) * (f.us + f.us_row * M);
       if (us < least) { least = us; best = {0, f.ns, 1}; }
     }
@@ -43,11 +45,14 @@ inline Fp4Split fp4_split(int M, int N, int K, int n_cu, float join, int most_sl
 }
 
 // As a call of its own; partial sums of a forward call, whose taker adds them up, in at most `room` floats (S 0: they do not fit);
-// and gate/up of a forward call, F columns of either.
+// and gate/up of a forward call, F columns of either.  Slices that nobody has to join leave the kernel for few rows one or two
+// rows of more than 32768 columns (on 256 CUs), four strips a workgroup.
 #define FP4_MOST_SLICES 16
+#define FP4_PARTS_FEW_ROWS 2
+#define FP4_PARTS_FEW_STRIPS 4
 inline Fp4Split fp4_split_call(int M, int N, int K, int n_cu) { return fp4_split(M, N, K, n_cu, 7.f, FP4_MOST_SLICES); }
 inline Fp4Split fp4_split_parts(int M, int N, int K, int n_cu, size_t room) {
-  Fp4Split f = fp4_split(M, N, K, n_cu, 0.f, FP4_MOST_SLICES);
+  Fp4Split f = fp4_split(M, N, K, n_cu, 0.f, FP4_MOST_SLICES, FP4_PARTS_FEW_ROWS, FP4_PARTS_FEW_STRIPS);
   while (f.S > 0 && (size_t)f.S * M * N > room) --f.S;
   return f;
 }

@@ -16,6 +16,11 @@ extern "C" void cut(int kind, int m, int n, int k, int n_cu, long room, int* o) 
                                                                            : fp4_split_gateup(m, n, k, n_cu);
   o[0] = f.mt; o[1] = f.ns; o[2] = f.S;
 }
+extern "C" int parts_free(int m, int n, int k, int n_cu, int* o) {
+  const Fp4Split f = fp4_split(m, n, k, n_cu, 0.f, FP4_MOST_SLICES);
+  o[0] = f.mt; o[1] = f.ns; o[2] = f.S;
+  return f.mt ? 0 : 1;
+}
 extern "C" long bytes(int n, int k) { return (long)fp4_bytes(n, k); }
 """
 CALL, PARTS, GATEUP = 0, 1, 2
@@ -95,3 +100,16 @@ def test_forward_calls_reach_every_kernel_and_its_loop(lib):
     want |= {(what, mt, ns, True, True) for mt, ns in TILED for what in ("parts", "gated")}
     want.add(("parts", 0, 4, False, True))          # one or two rows of more than 32768 columns
     assert want <= seen
+
+
+def test_partial_sums_have_the_kernel_for_few_rows_where_it_is_the_faster_one(lib):
+    """The kernels that partial sums do not have would be chosen nowhere: the cut is what it is with all of them."""
+    rng = np.random.default_rng(4)
+    n_few, free = 0, (C.c_int * 3)()
+    for i in range(20000):
+        m, units = int(rng.integers(1, 17 if i % 2 else 3)), int(2 ** rng.uniform(0, 9))
+        strips = int(rng.integers(2000, 3200)) if i % 4 == 0 else int(2 ** rng.uniform(0, 13))
+        n_cu = int(rng.choice([32, 64, 128, 256]))
+        n_few += lib.parts_free(m, strips * 16, units * 256, n_cu, free)
+        assert cut(lib, PARTS, m, strips * 16, units * 256, n_cu) == tuple(free), (m, units, strips, n_cu)
+    assert n_few > 100
