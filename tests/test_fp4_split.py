@@ -113,3 +113,39 @@ def test_partial_sums_have_the_kernel_for_few_rows_where_it_is_the_faster_one(li
         n_few += lib.parts_free(m, strips * 16, units * 256, n_cu, free)
         assert cut(lib, PARTS, m, strips * 16, units * 256, n_cu) == tuple(free), (m, units, strips, n_cu)
     assert n_few > 100
+
+
+PLAN_DRIVER = r"""
+#include <string.h>
+#include "sp_plan.h"
+extern "C" int chunks(int n, const int* rows, const int* spans, int n_q, int n_kv, long room) {
+  AttnPlan p;
+  memset(&p, 0, sizeof(p));
+  p.n_seg = n;
+  for (int i = 0; i < n; ++i) { p.seg_rows[i] = rows[i]; p.seg_P[i] = spans[i] - rows[i]; p.seg_T[i] = rows[i]; }
+  return attn_split_fp4(p, n_q, n_kv, 256, (size_t)room) ? p.any_split : -1;
+}
+"""
+
+
+def test_calls_that_are_to_be_cut_are(tmp_path):
+    from test_gpu_fp4_calls import CALLS, KINDS, KV, REPLAYED
+    (tmp_path / "driver.cpp").write_text(PLAN_DRIVER)
+    csrc = os.path.join(os.path.dirname(os.path.abspath(__file__)), "..", "paper_2504_04104_amd", "csrc")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-I", csrc, str(tmp_path / "driver.cpp"), "-o", str(tmp_path / "driver.so")], check=True)
+    plan = C.CDLL(str(tmp_path / "driver.so"))
+
+    def is_cut(rows, spans, nq=8, nkv=2, most=64):
+        rows, spans = zip(*sorted(zip(rows, spans), key=lambda p: -p[1]))
+        n = len(rows)
+        return plan.chunks(n, (C.c_int * n)(*rows), (C.c_int * n)(*spans), nq, nkv, C.c_long(most * nq * 32))
+    for sh, flags, _, _ in KINDS.values():
+        for name, reqs in CALLS.items():
+            if flags & KV:
+                assert is_cut([n for *_, n in reqs], [sum(r) for r in reqs], sh.n_q_heads, sh.n_kv_heads, 256) == name.startswith("cut")
+    for name, (flags, _, _, rows, contexts) in REPLAYED.items():
+        if flags & KV:                              # whatever request has which context
+            for turn in range(len(rows)):
+                spans = [contexts[(i + turn) % len(rows)] + max(rows) + 3 for i in range(len(rows))]
+                assert is_cut(rows, spans) == name.endswith("_cut")
+    assert is_cut([4], [6004], 32, 8) and is_cut([5], [7005], 32, 8)  # two captured graphs of one stage

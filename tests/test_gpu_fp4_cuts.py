@@ -6,7 +6,8 @@ import torch
 import paper_2504_04104_amd as sp
 import workloads as wl
 from fp4_cases import FORWARDS, PRODUCTS
-from fp4_reference import ancestors, random_tree, stage
+from fp4_layers import layer, matrix, tree
+from fp4_reference import random_tree, stage
 
 pytestmark = pytest.mark.gpu
 U, F = 2.0 ** -8, 2.0 ** -24                        # half a step of bf16 and of float32, relative to the value
@@ -17,16 +18,12 @@ def rnd(seed, *size, scale=1.0):
     return torch.randn(*size, generator=g, device="cuda", dtype=torch.bfloat16) * scale
 
 
-def held(p):
-    return sp.fp4_unpack_matrix(p).double()
-
-
 @pytest.mark.parametrize("m,n,k,gated", PRODUCTS)
 def test_product(m, n, k, gated):
     """Off by the result's rounding and float32 sums of k terms in any order: at most k * 2^-24 times the sum of their magnitudes.
     silu changes by at most 1.1 per unit, and its exponential and quotient are good to 2^-20."""
     x, p = rnd(m, m, k), sp.fp4_pack_matrix(rnd(n, n * (2 if gated else 1), k, scale=0.05))
-    y, w, xd = sp.fp4_product(x, p, gated=gated).double(), held(p), x.double()
+    y, w, xd = sp.fp4_product(x, p, gated=gated).double(), matrix(p), x.double()
     ref, mag = xd @ w.T, k * F * (xd.abs() @ w.abs().T)
     if gated:
         a, b, ea, eb = ref[:, :n], ref[:, n:], mag[:, :n], mag[:, n:]
@@ -34,34 +31,6 @@ def test_product(m, n, k, gated):
         ref, mag = s * b, 1.1 * ea * (b.abs() + eb) + s.abs() * eb + 2.0 ** -20 * (s * b).abs()
     assert y.shape == ref.shape
     assert ((y - ref).abs() <= U * ref.abs() + 1.01 * mag + 1e-30).all()
-
-
-def layer_reference(w, x, P, parents, k_old, v_old, sh, r):
-    """One layer in float64: rows x of a tree behind P rows of the cache.  r: what the rows between the products, the queries and
-    what the cache takes are rounded by."""
-    nq, kv, dh, n = sh.n_q_heads, sh.n_kv_heads, sh.d_head, len(x)
-
-    def norm(v, gain):
-        return r(v * torch.rsqrt(v.square().mean(-1, keepdim=True) + sh.rms_eps) * gain.double())
-    up = torch.from_numpy(ancestors(parents)).cuda()
-    pos = P + up.sum(1).double() - 1
-    ang = pos[:, None, None] * sh.rope_theta ** (-2.0 * torch.arange(dh // 2, device="cuda", dtype=torch.float64) / dh)
-
-    def rot(t):
-        a, b = t[..., :dh // 2], t[..., dh // 2:]
-        return r(torch.cat([a * ang.cos() - b * ang.sin(), b * ang.cos() + a * ang.sin()], -1))
-    qkv = (norm(x, w["norm1"]) @ held(w["wqkv"]).T).view(n, nq + 2 * kv, dh)
-    q, k = rot(qkv[:, :nq]), torch.cat([k_old.double(), rot(qkv[:, nq:nq + kv])])
-    v = torch.cat([v_old.double(), r(qkv[:, nq + kv:])])
-    seen = torch.cat([torch.ones(n, P, dtype=torch.bool, device="cuda"), up], 1)
-    att = torch.empty(n, nq, dh, dtype=torch.float64, device="cuda")
-    for h in range(nq):
-        c = h * kv // nq
-        s = (q[:, h] @ k[:, c].T.contiguous()) / dh ** 0.5
-        att[:, h] = r(torch.softmax(s.masked_fill(~seen, float("-inf")), -1) @ v[:, c])
-    h = x + att.view(n, nq * dh) @ held(w["wo"]).T
-    gu = norm(h, w["norm2"]) @ held(w["wgu"]).T
-    return h + r(torch.nn.functional.silu(gu[:, :sh.d_ff]) * gu[:, sh.d_ff:]) @ held(w["wd"]).T
 
 
 @pytest.mark.parametrize("d,nq,nkv,ff,m", FORWARDS)
@@ -84,6 +53,7 @@ def test_forward(d, nq, nkv, ff, m):
     st.tree_insert(0, parents)
     x = rnd(22, m, d)
     y = st.stage_forward([0], [0], [m], x).double()
-    ref = layer_reference(st.layers[0], x.double(), P, parents, k, v, sh, lambda t: t.to(torch.bfloat16).double())
+    pos, seen = tree(P, parents)
+    ref = layer(st.layers[0], x.double(), pos, seen, lambda kn, vn: (torch.cat([k.double(), kn]), torch.cat([v.double(), vn])), sh)
     assert (y - ref).abs().max() <= 1e-2 * ref.abs().max()
     assert ((y - x.double()) - (ref - x.double())).abs().max() <= 2e-2 * (ref - x.double()).abs().max()
