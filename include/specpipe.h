@@ -272,8 +272,9 @@ int sp_kv_load(sp_stage* stage, int32_t req, int32_t layer, int32_t first_slot, 
 
 /* Head norms: from here on the stage's query and key heads pass RMSNorm(x; gain, rms_eps) over their d_head columns, in
  * float32, before the rotation, in sp_stage_forward and sp_stage_append.  `layers` is a host array of n_layers entries holding
- * device pointers, which must stay valid; NULL: none (the state after sp_stage_create).  A set-up call: it may wait for the
- * device, and is not for use inside a stream capture.  Errors: SP_E_INVALID, SP_E_HIP. */
+ * device pointers, which must stay valid until others are set; NULL: none (the state after sp_stage_create).  A set-up call: it
+ * waits for the device where calls that read the gains of before may still run, and is not for use inside a stream capture.
+ * Errors: SP_E_INVALID, SP_E_HIP. */
 int sp_stage_set_head_norms(sp_stage* stage, const sp_head_norms* layers);
 
 /* ---- the hot path ------------------------------------------------------------ */

@@ -998,8 +998,8 @@ int sp_stage_set_head_norms(sp_stage* s, const sp_head_norms* layers) {
       if (!layers[l].q || !layers[l].k) return SP_E_INVALID;
       if (((uintptr_t)layers[l].q | (uintptr_t)layers[l].k) & 15) return SP_E_INVALID;
     }
-  // what was captured does not know these pointers (and may be running)
-  if (!s->graphs.empty()) {
+  // calls and replays that are still to run read the gains of before; what was captured does not know the new ones
+  if (!s->graphs.empty() || !s->norms.empty()) {
     const hipError_t e = hipDeviceSynchronize();
     if (e != hipSuccess) return hip_fail(s, e);
   }

@@ -216,6 +216,23 @@ def test_new_head_norms_are_those_of_the_next_call():
     assert not torch.equal(a, b) and not torch.equal(a, none)
 
 
+def test_gains_that_are_replaced_may_go():
+    """Calls that were made with them have run when the call returns, also those that no graph replays."""
+    use_own_stream()
+    st, _, gains = make(shape(8, 2, 128, 1, 512, 512), KV | sp.SP_FLAG_NO_GRAPHS, True, 0, 512, 1, 64)
+    st.request_init(0, 0, 300, 50)
+    st.tree_insert(0, [-1, 0])
+    big = torch.randn(8192, 8192, device="cuda", dtype=torch.bfloat16)
+    for norms in (None, gains, [{n: t + 1 for n, t in g.items()} for g in gains], gains):
+        had = st.head_norms is not None
+        for _ in range(40):                         # some 30 ms in front of the call
+            big @ big
+        st.stage_forward([0], [0], [2], rnd(1, 2, 512))
+        st.set_head_norms(norms)
+        assert torch.cuda.current_stream().query() or not had
+        torch.cuda.synchronize()
+
+
 # ---- products and pieces at the same time, and at the limits --------------------------------------------------------------
 def test_products_that_cut_their_columns_on_two_streams():
     """Each has a workspace, which the other must not write: other rows on either stream."""
