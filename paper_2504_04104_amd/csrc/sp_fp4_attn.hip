@@ -12,10 +12,11 @@
 //                 its share of P^T holds, converts pairs of columns of a slot (one instruction, the group's scale in it), and
 //                 exchanges halves of registers of neighbouring slots.
 //
-// What bounds it: few rows behind a short range, the launch and the code's first way through the instruction cache (one row
-// behind 500 slots 7.1 us); many rows, the issue of vector instructions, the conversions of V above all, which every block of 16
-// rows makes for itself (128 rows behind 8000 slots 27.6 us, 70 MB of it out of L2; 32 requests of 16-32 nodes behind 500-1000
-// slots 34); few rows behind a long range, memory and the second launch (one row behind 30000 slots, 32.6 MB, 14.5 us).
+// What bounds it: few rows behind a short range, latencies one after the other (one row behind 500 slots 7.1-7.9 us; how they
+// divide was not measured); many rows, the issue of vector instructions, the conversions of V above all, which every block of 16
+// rows makes for itself (128 rows behind 8000 slots 26.1-28.0 us, 70 MB of it out of L2; 32 requests of 16-32 nodes behind 500-1000
+// slots 34); few rows behind a long range, memory and the second launch (one row behind 30000 slots, 32.6 MB, 14.5 us; as a forward
+// call's launches 10.6-12.8 and 4.1-4.8).
 #include "sp_attn.h"
 #include "sp_fp4.h"
 
