@@ -277,6 +277,111 @@ int sp_kv_load(sp_stage* stage, int32_t req, int32_t layer, int32_t first_slot, 
  * Errors: SP_E_INVALID, SP_E_HIP. */
 int sp_stage_set_head_norms(sp_stage* stage, const sp_head_norms* layers);
 
+/* ---- rotary positions ----------------------------------------------------------
+ *
+ * Pair t < dims / 2 of a head's first `dims` columns, (t, t + dims / 2) in halves or (2t, 2t + 1) interleaved, turns at position p:
+ * (a, b) -> gain * (a cos - b sin, b cos + a sin) at the angle p * freq[t].  The other columns pass.  Angles are formed in double
+ * precision. */
+#define SP_ROPE_MAX_PAIRS 128
+typedef enum sp_rope_layout { SP_ROPE_HALVES = 0, SP_ROPE_INTERLEAVED = 1 } sp_rope_layout;
+typedef struct sp_rope {
+  int32_t layout;                    /* sp_rope_layout */
+  int32_t dims;                      /* rotated columns: a multiple of 8 */
+  float gain;                        /* of cosine and sine: 1, or what a long-context scaling asks for */
+  int32_t reserved;
+  double freq[SP_ROPE_MAX_PAIRS];    /* angle per position of the dims / 2 pairs */
+} sp_rope;
+
+/* Frequencies theta^(-2t / dims) of the pairs, scaled for contexts `factor` times as long as the `original` one:
+ *   SP_ROPE_PLAIN   as they are (factor, original, first, second are not looked at)
+ *   SP_ROPE_LINEAR  divided by factor (original, first, second are not looked at)
+ *   SP_ROPE_BANDS   by the turns a pair makes within the original context, original * freq / 2 pi: divided by factor up to `first`
+ *                   turns, as they are from `second` turns on, blended linearly by the turns in between (first < second)
+ *   SP_ROPE_RAMP    by the pair's number: with c(turns) = dims ln(original / (2 pi turns)) / (2 ln theta), as they are up to
+ *                   lo = max(floor(c(first)), 0), divided by factor from hi = min(ceil(c(second)), dims - 1) on (hi at least lo + 0.001),
+ *                   blended linearly by the number in between (first > second)
+ * Pure host arithmetic.  Errors: SP_E_INVALID (dims not a multiple of 8 in [8, 2 SP_ROPE_MAX_PAIRS], theta <= 1, factor < 1,
+ * original <= 0, first and second not positive or out of order). */
+typedef enum sp_rope_scaling { SP_ROPE_PLAIN = 0, SP_ROPE_LINEAR = 1, SP_ROPE_BANDS = 2, SP_ROPE_RAMP = 3 } sp_rope_scaling;
+int sp_rope_frequencies(int32_t dims, double theta, int32_t scaling, double factor, double original, double first, double second,
+                        double* freq_out /*host, dims / 2*/);
+
+/* Rows of heads rotated at positions of their own: x and out [n_rows][n_heads] of d_head columns (a multiple of 8, up to 256),
+ * strides between rows and between heads in elements, multiples of 8 and at least 0 (out: no two heads on the same elements);
+ * positions [n_rows] (device).  out may be x, with x's strides (in place), and may not overlap it otherwise, from its first element
+ * to its last.  inverse = 1 turns
+ * back by the same angles with the same gain: the transpose, by which gradients come back.  Pointers are 16-byte aligned device
+ * memory.  Keys for sp_kv_store are rotated with it, and what a stage does not compute.  n_rows == 0 does nothing.  Errors: SP_E_INVALID,
+ * SP_E_UNSUPPORTED (d_head, strides). */
+int sp_rotate(const sp_rope* rope, int32_t dtype, int32_t inverse, const void* x, int64_t x_row, int64_t x_head, int32_t n_rows,
+              int32_t n_heads, int32_t d_head, const int32_t* positions /*device*/, void* out, int64_t out_row, int64_t out_head,
+              sp_stream stream);
+
+/* From here on the stage's query and key heads are rotated so, in sp_stage_forward, sp_stage_append and sp_latent_append; NULL: as after
+ * sp_stage_create, whole heads in halves at theta^(-2t / d_head) (a latent stage: its d_rope columns).  dims up to d_head (d_rope), of
+ * which at most 128 are rotated.  Rows that the cache holds already are not touched.  A set-up call: it waits for the device where
+ * calls of before may still be replayed, and is not for use inside a stream capture; what the caller has captured keeps the rotation of
+ * its time.  Errors: SP_E_INVALID, SP_E_UNSUPPORTED (a cache in 4 bits: halves of a part that is no multiple of 64 columns),
+ * SP_E_HIP. */
+int sp_stage_set_rope(sp_stage* stage, const sp_rope* rope /*host, nullable*/);
+
+/* ---- a cache of latent vectors --------------------------------------------------------
+ *
+ * Models whose keys and values come from one shared vector a token: key_h = [W_k,h c | r], value_h = W_v,h c, with the latent c
+ * (d_latent values) and a rotated part r (d_rope) that all heads share.  The cache holds [c | r], one row a token and layer; queries go
+ * into the latent space, q_h -> [W_k,h^T q_h | rotated part of q_h] (sp_head_product, sp_latent_append), attention runs there, every
+ * head over the same rows, and its results come out by W_v,h (sp_head_product).
+ *
+ * A latent stage is a stage with such a cache, for models whose other parts the caller computes.  In its sp_config: dtype SP_BF16,
+ * n_kv_heads 1, d_head = d_latent + d_rope, rope_theta and rms_eps as ever, d_ff not looked at, flags SP_FLAG_PAGED_KV and
+ * SP_FLAG_SIMPLE_KERNELS; d_model is that of hidden rows (sp_kv_compact, verification).  Matrix-core kernels cover d_latent 256 and 512 with
+ * d_rope 32 and 64, plain ones every multiple of 8 up to 1024 and 128.  The slab is [layer][slot][d_latent + d_rope].
+ * Requests, trees, pruning, compaction, pages and verification (the output head; vocabulary matrix row-major) are those of every stage;
+ * sp_stage_forward, sp_stage_append, sp_stage_attention, sp_kv_store, sp_kv_load and sp_stage_set_head_norms return SP_E_UNSUPPORTED,
+ * as the sp_latent_ calls do on other stages. */
+typedef struct sp_latent {
+  int32_t d_latent;
+  int32_t d_rope;
+  float scale;                  /* of the scores, e.g. 1 / sqrt of a whole key's length; > 0 */
+  int32_t reserved;
+  const void* const* norms;     /* host array of n_layers device pointers to [d_latent] bf16 gains of the latents' RMSNorm (16-byte
+                                 * aligned, valid until sp_stage_destroy), or NULL: none */
+} sp_latent;
+int sp_latent_query_sizes(const sp_config* cfg, const sp_latent* latent, sp_sizes* out);
+int sp_latent_stage_create(const sp_config* cfg, const sp_latent* latent, const sp_buffers* buffers, sp_stream stream, sp_stage** out);
+
+/* Rows [n][d_latent + d_rope] (bf16, 16-byte aligned device memory) stored into, or read from, the logical slots first_slot ..
+ * first_slot + n - 1 of one layer, as they are (normed, rotated).  Errors as sp_kv_store's. */
+int sp_latent_store(sp_stage* stage, int32_t req, int32_t layer, int32_t first_slot, int32_t n, const void* rows, sp_stream stream);
+int sp_latent_load(sp_stage* stage, int32_t req, int32_t layer, int32_t first_slot, int32_t n, void* rows, sp_stream stream);
+
+/* One layer's rows on their way in, the same rows, order and errors as sp_stage_append, in one launch.
+ * kv [sum n_nodes] of d_latent + d_rope columns: the latent is normed where the stage has norms, the rest rotated at prefix_len + depth,
+ * and both go to the node's cache slot.  q [sum n_nodes][n_q_heads] of d_rope columns, the query heads' parts to rotate, go rotated to
+ * q_out (for instance to the last columns of the queries that sp_latent_attention takes).  Strides between rows and heads in elements,
+ * multiples of 8 and at least 0 (q_out: no two heads on the same elements); q_out may be q, with q's strides, and may not overlap q or kv
+ * otherwise, from its first element to its last.  Appending to the stage's last layer makes the nodes count as forwarded. */
+int sp_latent_append(sp_stage* stage, int32_t layer, int32_t n_req, const int32_t* req_ids /*host*/, const int32_t* first_node /*host*/,
+                     const int32_t* n_nodes /*host*/, const void* q, int64_t q_row, int64_t q_head, const void* kv, int64_t kv_row,
+                     void* q_out, int64_t out_row, int64_t out_head, sp_stream stream);
+
+/* Tree attention of one layer in the latent space, the same rows, order and errors as sp_stage_attention: q [sum n_nodes][n_q_heads][d_latent +
+ * d_rope], out [sum n_nodes][n_q_heads][d_latent] = softmax(scale * q . row) over the rows of the committed context, the node itself and
+ * its ancestors, times those rows' latents.  Sums and softmax statistics are float32; the softmax's weights are rounded to bf16 before
+ * they meet the latents, and divided by the sum of the rounded ones.  q and out are 16-byte aligned device memory and may not overlap.
+ * Uses the stage's workspace. */
+int sp_latent_attention(sp_stage* stage, int32_t layer, int32_t n_req, const int32_t* req_ids /*host*/,
+                        const int32_t* first_node /*host*/, const int32_t* n_nodes /*host*/, const void* q, void* out, sp_stream stream);
+
+/* Products head by head, bf16 with float32 sums: out[i][h] = x[i][h] W[h]^T with x [m][heads] of k columns, W [heads][n][k], out
+ * [m][heads] of n columns; any m, also a single row.  Strides between rows and heads in elements, multiples of 8 and at least 0 (out:
+ * no two heads on the same elements); k % 32 == 0 and n % 16 == 0, both up to SP_HEAD_PRODUCT_MAX.  Pointers are 16-byte aligned device
+ * memory; out may not overlap x, from its first element to its last.  m == 0 does nothing.  Errors: SP_E_INVALID, SP_E_UNSUPPORTED
+ * (shape, strides). */
+#define SP_HEAD_PRODUCT_MAX 4096
+int sp_head_product(const void* x, int64_t x_row, int64_t x_head, int32_t m, int32_t heads, const void* w, int32_t n, int32_t k, void* out,
+                    int64_t out_row, int64_t out_head, sp_stream stream);
+
 /* ---- the hot path ------------------------------------------------------------ */
 
 /* Layer appending (Sec. 3.2): appends n_new nodes to request `req`.  parents[k] is

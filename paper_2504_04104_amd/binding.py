@@ -82,6 +82,21 @@ class sp_head_weights(C.Structure):
     _fields_ = [("norm", C.c_void_p), ("wvocab", C.c_void_p), ("vocab", C.c_int32), ("reserved", C.c_int32)]
 
 
+SP_ROPE_MAX_PAIRS = 128
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"linear": 1, "bands": 2, "ramp": 3}
+
+
+class sp_rope(C.Structure):
+    _fields_ = [("layout", C.c_int32), ("dims", C.c_int32), ("gain", C.c_float), ("reserved", C.c_int32),
+                ("freq", C.c_double * SP_ROPE_MAX_PAIRS)]
+
+
+class sp_latent(C.Structure):
+    _fields_ = [("d_latent", C.c_int32), ("d_rope", C.c_int32), ("scale", C.c_float), ("reserved", C.c_int32),
+                ("norms", C.POINTER(C.c_void_p))]
+
+
 _lib = None
 
 
@@ -114,6 +129,17 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
         # (host arrays as addresses: a pointer object for each costs these short calls 0.3 us)
         "sp_stage_append": [vp, C.c_int32, C.c_int32, vp, vp, vp, vp, vp, vp],
         "sp_stage_attention": [vp, C.c_int32, C.c_int32, vp, vp, vp, vp, vp, vp],
+        "sp_rope_frequencies": [C.c_int32, C.c_double, C.c_int32, C.c_double, C.c_double, C.c_double, C.c_double, C.POINTER(C.c_double)],
+        "sp_rotate": [C.POINTER(sp_rope), C.c_int32, C.c_int32, vp, C.c_int64, C.c_int64, C.c_int32, C.c_int32, C.c_int32, vp, vp, C.c_int64,
+                      C.c_int64, vp],
+        "sp_stage_set_rope": [vp, C.POINTER(sp_rope)],
+        "sp_latent_query_sizes": [C.POINTER(sp_config), C.POINTER(sp_latent), C.POINTER(sp_sizes)],
+        "sp_latent_stage_create": [C.POINTER(sp_config), C.POINTER(sp_latent), C.POINTER(sp_buffers), vp, C.POINTER(vp)],
+        "sp_latent_store": [vp, C.c_int32, C.c_int32, C.c_int32, C.c_int32, vp, vp],
+        "sp_latent_load": [vp, C.c_int32, C.c_int32, C.c_int32, C.c_int32, vp, vp],
+        "sp_latent_append": [vp, C.c_int32, C.c_int32, vp, vp, vp, vp, C.c_int64, C.c_int64, vp, C.c_int64, vp, C.c_int64, C.c_int64, vp],
+        "sp_latent_attention": [vp, C.c_int32, C.c_int32, vp, vp, vp, vp, vp, vp],
+        "sp_head_product": [vp, C.c_int64, C.c_int64, C.c_int32, C.c_int32, vp, C.c_int32, C.c_int32, vp, C.c_int64, C.c_int64, vp],
         "sp_request_init": [vp, C.c_int32, C.c_int64, C.c_int32, C.c_int32, vp],
         "sp_stage_verify_head": [vp, C.POINTER(sp_head_weights), C.c_int32, i32p, i32p, i32p, vp, vp, vp, vp],
         "sp_stage_verify_head_noalloc": [vp, C.POINTER(sp_head_weights), C.c_int32, i32p, i32p, i32p, vp, vp, vp, vp],
@@ -212,6 +238,32 @@ def _matrix_shape(shape, name: str):
 def _check(rc: int, what: str):
     if rc != 0:
         raise SpError(rc, what)
+
+
+class Rope:
+    """Rotary positions (sp_rope): layout "half" (pairs t, t + dims / 2) or "interleaved" (2t, 2t + 1) of a head's first dims columns.
+    scaling: None, ("linear", factor), ("bands", factor, original, first, second) or ("ramp", factor, original, first, second), as
+    sp_rope_frequencies has them; or freq, dims / 2 angles per position, in place of theta and scaling."""
+
+    def __init__(self, layout: str, dims: int, theta: float = 0.0, scaling: Optional[tuple] = None, gain: float = 1.0,
+                 freq: Optional[Sequence[float]] = None):
+        self.c = sp_rope(ROPE_LAYOUTS[layout], dims, gain, 0)
+        if freq is not None:
+            if len(freq) * 2 != dims or len(freq) > SP_ROPE_MAX_PAIRS:
+                raise SpError(-1, "a rotation of %d columns at %d frequencies" % (dims, len(freq)))
+            self.c.freq[:len(freq)] = [float(f) for f in freq]
+            return
+        kind, args = 0, (1.0, 1.0, 1.0, 1.0)
+        if scaling is not None:
+            kind, args = ROPE_SCALINGS[scaling[0]], tuple(scaling[1:])
+            if len(args) != (1 if kind == 1 else 4):
+                raise ValueError("scaling %r" % (scaling,))
+            args = (args + (1.0, 1.0, 1.0))[:4]
+        _check(load_library().sp_rope_frequencies(dims, theta, kind, *args, self.c.freq), "sp_rope_frequencies")
+
+    @property
+    def freq(self) -> List[float]:
+        return self.c.freq[:self.c.dims // 2]
 
 
 class Stage:
@@ -364,6 +416,10 @@ class Stage:
                     setattr(arr[l], name, t.data_ptr())
         _check(self.lib.sp_stage_set_head_norms(self.handle, arr), "sp_stage_set_head_norms")
         self.head_norms = norms                  # keeps the gains alive
+
+    def set_rope(self, rope: Optional[Rope]):
+        """sp_stage_set_rope: the rotation of the stage's query and key heads from here on; None: as created."""
+        _check(self.lib.sp_stage_set_rope(self.handle, None if rope is None else C.byref(rope.c)), "sp_stage_set_rope")
 
     def _rows_at(self, t, rows: int, cols: int) -> int:
         assert t.is_cuda and t.dtype is self.tdtype and t.dim() == 2 and t.shape[0] == rows and t.shape[1] == cols and t.is_contiguous()
@@ -747,6 +803,154 @@ def fp4_product(x, w: Fp4Matrix, gated: bool = False, out=None):
     _check(lib.sp_fp4_product(x.data_ptr(), m, w.data.data_ptr(), n, k, 1 if gated else 0, out.data_ptr(), work.data_ptr() if size else None,
                               size, torch._C._cuda_getCurrentRawStream(device.index)), "sp_fp4_product")
     return out
+
+
+# ---- rotary positions and products head by head ---------------------------------------------
+def _heads(t, rows: int, heads: int, cols: int, dtype, device) -> tuple:
+    """(address, row stride, head stride) of [rows, heads, cols] whose heads lie one element after the other."""
+    assert t.is_cuda and t.device == device and t.dtype is dtype and t.dim() == 3
+    assert t.shape[0] == rows and t.shape[1] == heads and t.shape[2] == cols and t.stride(2) == 1
+    # (the stride of an axis of one entry says nothing: torch's may be anything)
+    return t.data_ptr(), t.stride(0) if rows > 1 else 0, t.stride(1) if heads > 1 else 0
+
+
+def rotate(x, positions, rope: Rope, inverse: bool = False, out=None):
+    """sp_rotate: x [rows, heads, d_head] (bf16 or float32, rows and heads of any stride) turned at positions [rows] (int32, on x's
+    device); inverse: back, by which gradients come back.  out may be x."""
+    import torch
+    device = x.device
+    assert x.is_cuda and positions.device == device
+    if device.index != torch._C._cuda_getDevice():
+        with torch.cuda.device(device):
+            return rotate(x, positions, rope, inverse, out)
+    rows, heads, d = x.shape
+    assert x.dtype in (torch.bfloat16, torch.float32)
+    assert positions.dtype is torch.int32 and positions.shape == (rows,) and positions.is_contiguous()
+    if out is None:
+        out = torch.empty(rows, heads, d, dtype=x.dtype, device=device)
+    _check(load_library().sp_rotate(C.byref(rope.c), SP_BF16 if x.dtype is torch.bfloat16 else SP_F32, 1 if inverse else 0,
+                                    *_heads(x, rows, heads, d, x.dtype, device), rows, heads, d, positions.data_ptr(),
+                                    *_heads(out, rows, heads, d, x.dtype, device), torch._C._cuda_getCurrentRawStream(device.index)), "sp_rotate")
+    return out
+
+
+def head_product(x, w, out=None):
+    """sp_head_product: x [m, heads, k] bf16 (rows and heads of any stride) times w [heads, n, k], head by head: [m, heads, n]."""
+    import torch
+    device = x.device
+    assert x.is_cuda and w.device == device
+    if device.index != torch._C._cuda_getDevice():
+        with torch.cuda.device(device):
+            return head_product(x, w, out)
+    m, heads, k = x.shape
+    n = w.shape[1]
+    assert w.dtype is torch.bfloat16 and w.shape == (heads, n, k) and w.is_contiguous()
+    if out is None:
+        out = torch.empty(m, heads, n, dtype=torch.bfloat16, device=device)
+    xp, xr, xh = _heads(x, m, heads, k, torch.bfloat16, device)
+    _check(load_library().sp_head_product(xp, xr, xh, m, heads, w.data_ptr(), n, k, *_heads(out, m, heads, n, torch.bfloat16, device),
+                                          torch._C._cuda_getCurrentRawStream(device.index)), "sp_head_product")
+    return out
+
+
+# ---- a cache of latent vectors --------------------------------------------------------------
+class LatentStage(Stage):
+    """A stage whose cache holds one row of d_latent + d_rope bf16 values a token and layer (sp_latent_stage_create).  Requests, trees,
+    pruning, compaction, pages and verification are Stage's; forward calls are not offered.  scale: of the scores.  norms: per layer
+    the gain [d_latent] of the latents' RMSNorm, or None.  rope: of the shared key part and of the query heads' (default: all d_rope
+    columns in halves at rope_theta)."""
+
+    def __init__(self, n_layers: int, n_heads: int, d_latent: int, d_rope: int, *, scale: float, kv_slots: int, rms_eps: float = 1e-6,
+                 rope_theta: float = 10000.0, rope: Optional[Rope] = None, norms: Optional[List["object"]] = None, d_model: int = 256,
+                 max_requests: int = 1, max_batch_nodes: int = 64, max_tree_nodes: int = SP_MAX_TREE_NODES, page_slots: int = 0,
+                 flags: int = 0, device: str = "cuda:0"):
+        import torch
+        self.torch, self.lib, self.handle = torch, load_library(), None
+        self.device, self.dtype, self.tdtype = torch.device(device), SP_BF16, torch.bfloat16
+        self.n_layers, self.n_heads, self.d_latent, self.d_rope, self.page_slots = n_layers, n_heads, d_latent, d_rope, page_slots
+        if page_slots:
+            flags |= SP_FLAG_PAGED_KV
+        self.cfg = sp_config(n_layers, d_model, n_heads, 1, d_latent + d_rope, 8, rms_eps, rope_theta, SP_BF16, max_requests, max_tree_nodes,
+                             max_batch_nodes, kv_slots, flags, page_slots)
+        lat = sp_latent(d_latent, d_rope, scale, 0, None)
+        if norms is not None:
+            assert len(norms) == n_layers
+            for t in norms:
+                assert t.is_cuda and t.is_contiguous() and t.dtype == torch.bfloat16 and t.shape == (d_latent,)
+            lat.norms = (C.c_void_p * n_layers)(*[t.data_ptr() for t in norms])
+        self.norms = norms                       # keeps the gains alive
+        sz = sp_sizes()
+        _check(self.lib.sp_latent_query_sizes(C.byref(self.cfg), C.byref(lat), C.byref(sz)), "sp_latent_query_sizes")
+        self.sizes = sz
+        h = C.c_void_p()
+        with torch.cuda.device(self.device):
+            self.kv = torch.zeros(sz.kv_bytes, dtype=torch.uint8, device=self.device)
+            self.tables = torch.zeros(sz.tables_bytes, dtype=torch.uint8, device=self.device)
+            self.workspace = torch.zeros(sz.workspace_bytes, dtype=torch.uint8, device=self.device)
+            bufs = sp_buffers(self.kv.data_ptr(), sz.kv_bytes, self.tables.data_ptr(), sz.tables_bytes, self.workspace.data_ptr(), sz.workspace_bytes)
+            _check(self.lib.sp_latent_stage_create(C.byref(self.cfg), C.byref(lat), C.byref(bufs), self._stream(), C.byref(h)), "sp_latent_stage_create")
+        self.handle = h
+        if rope is not None:
+            self.set_rope(rope)
+
+    def _elsewhere(self) -> bool:
+        return self.device.index is not None and self.device.index != self.torch._C._cuda_getDevice()
+
+    def kv_view(self):
+        """The slab as a tensor [layer, slot, d_latent + d_rope] (no copy)."""
+        return self.kv.view(self.tdtype).view(self.n_layers, self.cfg.kv_slots, self.d_latent + self.d_rope)
+
+    def stage_forward(self, *args, **kwargs):
+        raise SpError(-9, "a forward call of a latent stage")
+
+    def set_head_norms(self, norms):
+        raise SpError(-9, "head norms of a latent stage")
+
+    def kv_store(self, req: int, layer: int, first_slot: int, rows):
+        """sp_latent_store: rows [n, d_latent + d_rope] into logical slots first_slot .. first_slot + n - 1."""
+        n = int(rows.shape[0])
+        _check(self.lib.sp_latent_store(self.handle, req, layer, first_slot, n, self._rows_at(rows, n, self.d_latent + self.d_rope), self._stream()),
+               "sp_latent_store")
+
+    def kv_load(self, req: int, layer: int, first_slot: int, n: int):
+        """sp_latent_load: the rows [n, d_latent + d_rope] that the cache holds."""
+        rows = self.torch.empty(max(n, 0), self.d_latent + self.d_rope, dtype=self.tdtype, device=self.device)
+        _check(self.lib.sp_latent_load(self.handle, req, layer, first_slot, n, rows.data_ptr(), self._stream()), "sp_latent_load")
+        return rows
+
+    def append(self, layer: int, req_ids: Sequence[int], first_node: Sequence[int], n_nodes: Sequence[int], q, kv, q_out=None):
+        """sp_latent_append: q [sum n_nodes, n_heads, d_rope] (a view: rows and heads of any stride) is rotated into q_out (default: a new
+        tensor); kv [sum n_nodes, d_latent + d_rope] (rows of any stride) goes to the nodes' cache slots."""
+        if self._elsewhere():
+            with self.torch.cuda.device(self.device):
+                return self.append(layer, req_ids, first_node, n_nodes, q, kv, q_out)
+        r, n, rows = self._counted(req_ids, n_nodes)
+        f = _ids(first_node)
+        assert len(f) == len(r)
+        if q_out is None:
+            q_out = self.torch.empty(max(rows, 0), self.n_heads, self.d_rope, dtype=self.tdtype, device=self.device)
+        at = kv.device
+        assert kv.is_cuda and kv.dtype is self.tdtype and kv.shape == (rows, self.d_latent + self.d_rope) and kv.stride(1) == 1
+        _check(self.lib.sp_latent_append(self.handle, layer, len(r), _at(r), _at(f), _at(n), *_heads(q, rows, self.n_heads, self.d_rope, self.tdtype, at),
+                                         kv.data_ptr(), kv.stride(0) if rows > 1 else 0,
+                                         *_heads(q_out, rows, self.n_heads, self.d_rope, self.tdtype, at), self._stream()), "sp_latent_append")
+        return q_out
+
+    def attention(self, layer: int, req_ids: Sequence[int], first_node: Sequence[int], n_nodes: Sequence[int], q, out=None):
+        """sp_latent_attention: q [sum n_nodes, n_heads, d_latent + d_rope] -> [sum n_nodes, n_heads, d_latent]."""
+        if self._elsewhere():
+            with self.torch.cuda.device(self.device):
+                return self.attention(layer, req_ids, first_node, n_nodes, q, out)
+        r, n, rows = self._counted(req_ids, n_nodes)
+        f = _ids(first_node)
+        assert len(f) == len(r)
+        if out is None:
+            out = self.torch.empty(max(rows, 0), self.n_heads, self.d_latent, dtype=self.tdtype, device=self.device)
+        for t, cols in ((q, self.d_latent + self.d_rope), (out, self.d_latent)):
+            assert t.is_cuda and t.dtype is self.tdtype and t.shape == (rows, self.n_heads, cols) and t.is_contiguous()
+        _check(self.lib.sp_latent_attention(self.handle, layer, len(r), _at(r), _at(f), _at(n), q.data_ptr(), out.data_ptr(), self._stream()),
+               "sp_latent_attention")
+        return out
 
 
 # ---- data preparation helpers (layout only) ---------------------------------------------

@@ -55,6 +55,28 @@ struct Workspace {
 
 inline int elt_bytes(int dtype) { return dtype == SP_BF16 ? 2 : 4; }
 
+// Partial rows that the latent attention's cuts may take (sp_latent_plan.h): of every request's query rows as many as blocks cut into chunks
+// for all CUs hold.
+constexpr size_t LATENT_UNITS = 40960;
+
+// The workspace of a latent stage: the output head's and the attention's.
+Workspace carve_latent(const sp_config& c, int d_latent, char* base) {
+  Workspace w;
+  const size_t MB = align_up((size_t)c.max_batch_nodes, 16);
+  size_t off = 0;
+  auto take = [&](size_t bytes) { char* p = base ? base + off : nullptr; off += align_up(bytes); return (void*)p; };
+  w.rows = (RowInfo*)take(MB * sizeof(RowInfo));
+  w.cs = (float*)take(MB * 64 * sizeof(float));
+  w.h = (float*)take(MB * c.d_model * sizeof(float));
+  w.xn = take(MB * c.d_model * 2);
+  w.part_floats = (MB > 1024 ? MB : 1024) * (size_t)c.d_model;
+  w.part = (float*)take(w.part_floats * sizeof(float));
+  w.attn_units = LATENT_UNITS;
+  w.attn_part = (float*)take(w.attn_units * (size_t)(d_latent + 2) * sizeof(float));
+  w.total = off;
+  return w;
+}
+
 // Lays the workspace out from `base` (may be null: sizes only).
 Workspace carve(const sp_config& c, char* base) {
   Workspace w;
@@ -87,6 +109,33 @@ Workspace carve(const sp_config& c, char* base) {
   return w;
 }
 
+int check_pages(const sp_config& c) {
+  if (c.flags & SP_FLAG_PAGED_KV) {
+    // a page holds whole 32-slot attention tiles
+    const int pg = c.page_slots;
+    if (pg < 32 || pg > 4096 || (pg & (pg - 1))) return SP_E_INVALID;
+    if (c.kv_slots % pg) return SP_E_INVALID;
+  }
+  return SP_OK;
+}
+
+int check_latent(const sp_config* c, const sp_latent* l) {
+  if (!c || !l) return SP_E_INVALID;
+  if (c->n_layers < 1 || c->d_model < 8 || c->n_q_heads < 1 || c->n_kv_heads != 1 || l->d_latent < 8 || l->d_rope < 8) return SP_E_INVALID;
+  if ((int64_t)c->d_head != (int64_t)l->d_latent + l->d_rope) return SP_E_INVALID;
+  if (c->dtype != SP_F32 && c->dtype != SP_BF16) return SP_E_INVALID;
+  if (c->max_requests < 1 || c->max_tree_nodes < 1 || c->max_tree_nodes > SP_MAX_TREE_NODES) return SP_E_INVALID;
+  if (c->max_batch_nodes < 1 || c->kv_slots < 1) return SP_E_INVALID;
+  if (!(c->rms_eps > 0.f) || !(c->rope_theta > 1.f) || !(l->scale > 0.f) || !std::isfinite(l->scale)) return SP_E_INVALID;
+  if (c->flags & ~(SP_FLAG_PAGED_KV | SP_FLAG_SIMPLE_KERNELS | SP_FLAG_NO_GRAPHS)) return SP_E_UNSUPPORTED;
+  if (c->dtype != SP_BF16 || c->d_model % 8 || c->n_q_heads > 1024) return SP_E_UNSUPPORTED;
+  if (l->d_latent % 8 || l->d_latent > 1024 || l->d_rope % 8 || l->d_rope > 2 * SP_ROPE_PAIRS || c->kv_slots > 0x7fffffff) return SP_E_UNSUPPORTED;
+  if (l->norms)
+    for (int i = 0; i < c->n_layers; ++i)
+      if (!l->norms[i] || ((uintptr_t)l->norms[i] & 15)) return SP_E_INVALID;
+  return check_pages(*c);
+}
+
 int check_config(const sp_config* c) {
   if (!c) return SP_E_INVALID;
   if (c->n_layers < 1 || c->d_model < 8 || c->n_q_heads < 1 || c->n_kv_heads < 1 || c->d_ff < 8) return SP_E_INVALID;
@@ -100,13 +149,30 @@ int check_config(const sp_config* c) {
   if ((c->flags & (SP_FLAG_FP4_KV | SP_FLAG_FP4_WEIGHTS)) && c->dtype != SP_BF16) return SP_E_UNSUPPORTED;
   if ((c->flags & SP_FLAG_FP4_WEIGHTS) && (c->flags & SP_FLAG_PACKED_WEIGHTS)) return SP_E_INVALID;
   if ((c->flags & SP_FLAG_FP4_KV) && c->kv_slots > SP_FP4_MAX_SLOTS) return SP_E_UNSUPPORTED;
-  if (c->flags & SP_FLAG_PAGED_KV) {
-    // a page holds whole 32-slot attention tiles
-    const int pg = c->page_slots;
-    if (pg < 32 || pg > 4096 || (pg & (pg - 1))) return SP_E_INVALID;
-    if (c->kv_slots % pg) return SP_E_INVALID;
+  return check_pages(*c);
+}
+
+// The rotation of whole parts of `cols` columns in halves at the config's theta.
+StageRope plain_rope(int cols) {
+  StageRope r;
+  std::memset(&r, 0, sizeof(r));
+  r.gain = 1.f;
+  r.dims = cols;
+  return r;
+}
+
+// Rows of heads of `width` elements: from the first element to behind the last, in elements; -1: strides that are none, or (apart)
+// heads that share elements.
+int64_t strided_extent(int64_t rows, int64_t row, int64_t heads, int64_t head, int64_t width, bool apart) {
+  const int64_t most = (int64_t)1 << 31;
+  if (row < 0 || head < 0 || row >= most || head >= most || row % 8 || head % 8) return -1;
+  if (apart) {
+    const int64_t s0 = row < head ? row : head, n0 = row < head ? rows : heads, s1 = row < head ? head : row, n1 = row < head ? heads : rows;
+    if (n0 > 1 && s0 < width) return -1;
+    const int64_t inner = n0 > 1 ? (n0 - 1) * s0 + width : width;
+    if (n1 > 1 && s1 < inner) return -1;
   }
-  return SP_OK;
+  return (rows - 1) * row + (heads - 1) * head + width;
 }
 
 inline bool is_fp4_kv(const sp_config& c) { return (c.flags & SP_FLAG_FP4_KV) != 0; }
@@ -133,6 +199,11 @@ struct sp_stage {
   sp_config cfg;
   std::vector<sp_layer_weights> W;
   std::vector<sp_head_norms> norms;   // empty: the model has none
+  bool latent = false;                // a cache of latent vectors
+  LatentDims lat = {0, 0, 0};
+  float lat_scale = 0.f;
+  std::vector<const void*> lat_norms; // empty: the model has none
+  StageRope rope;
   sp_buffers buf;
   sp_sizes sizes;
   ReqMeta* d_meta = nullptr;
@@ -334,40 +405,53 @@ int sp_stage_query_sizes(const sp_config* cfg, sp_sizes* out) {
   return SP_OK;
 }
 
-int sp_stage_create(const sp_config* cfg, const sp_layer_weights* layers, const sp_buffers* buffers,
-                    sp_stream stream, sp_stage** out) {
-  int rc = check_config(cfg);
+int sp_latent_query_sizes(const sp_config* cfg, const sp_latent* latent, sp_sizes* out) {
+  const int rc = check_latent(cfg, latent);
   if (rc != SP_OK) return rc;
-  if (!layers || !buffers || !out) return SP_E_INVALID;
-  sp_sizes sz;
-  sp_stage_query_sizes(cfg, &sz);
+  if (!out) return SP_E_INVALID;
+  out->kv_row_bytes = (size_t)cfg->d_head * 2;
+  out->kv_plane_bytes = (size_t)cfg->kv_slots * out->kv_row_bytes;
+  out->kv_bytes = (size_t)cfg->n_layers * out->kv_plane_bytes;
+  out->tables_bytes = tables_meta_bytes(*cfg) + align_up((size_t)cfg->max_requests * sizeof(ReqTables)) + page_table_bytes(*cfg);
+  out->workspace_bytes = carve_latent(*cfg, latent->d_latent, nullptr).total;
+  return SP_OK;
+}
+
+// What every stage has: buffers, tables, pages, the device.  sz: what the buffers have to hold at least.
+static int make_stage(const sp_config* cfg, const sp_sizes& sz, const sp_buffers* buffers, sp_stage** out) {
   if (!buffers->kv || !buffers->tables || !buffers->workspace) return SP_E_INVALID;
   if (buffers->kv_bytes < sz.kv_bytes || buffers->tables_bytes < sz.tables_bytes ||
       buffers->workspace_bytes < sz.workspace_bytes)
     return SP_E_CAPACITY;
   if (((uintptr_t)buffers->kv | (uintptr_t)buffers->tables | (uintptr_t)buffers->workspace) & 255) return SP_E_INVALID;
-  for (int l = 0; l < cfg->n_layers; ++l) {
-    const sp_layer_weights& w = layers[l];
-    if (!w.wqkv || !w.wo || !w.wgu || !w.wd || !w.norm1 || !w.norm2) return SP_E_INVALID;
-    if (((uintptr_t)w.wqkv | (uintptr_t)w.wo | (uintptr_t)w.wgu | (uintptr_t)w.wd) & 15) return SP_E_INVALID;
+  int dev = 0, cus = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= SP_NOALLOC_MAX_DEVICES) return SP_E_HIP;
+  if (!g_noalloc_scratch[dev]) {
+    // this device's copy of the static scratch array (the device is current here)
+    void* p = nullptr;
+    if (hipGetSymbolAddress(&p, HIP_SYMBOL(sp_noalloc_scratch)) != hipSuccess || !p) return SP_E_HIP;
+    g_noalloc_scratch[dev] = p;
   }
   sp_stage* s = new (std::nothrow) sp_stage();
   if (!s) return SP_E_INVALID;
   s->cfg = *cfg;
-  s->W.assign(layers, layers + cfg->n_layers);
   s->buf = *buffers;
   s->sizes = sz;
+  s->device = dev;
+  if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && cus > 0)
+    s->n_cu = cus;
   s->d_meta = (ReqMeta*)buffers->tables;
   s->d_tables = (ReqTables*)((char*)buffers->tables + tables_meta_bytes(*cfg));
-  s->ws = carve(*cfg, (char*)buffers->workspace);
   s->geom.kv = (char*)buffers->kv;
   s->geom.plane_bytes = sz.kv_plane_bytes;
   s->geom.row_bytes = (int)sz.kv_row_bytes;
   s->geom.n_layers = cfg->n_layers;
   s->geom.n_kv_heads = cfg->n_kv_heads;
+  s->geom.planes = cfg->n_layers * 2 * cfg->n_kv_heads;
   s->geom.page_table = nullptr; s->geom.pt_stride = 0; s->geom.pg_shift = 0;
-  s->geom.scale_plane_bytes = scale_plane_bytes(*cfg);
-  s->geom.scales = is_fp4_kv(*cfg) ? s->geom.kv + (size_t)cfg->n_layers * 2 * cfg->n_kv_heads * sz.kv_plane_bytes : nullptr;
+  s->geom.scale_plane_bytes = 0;
+  s->geom.scales = nullptr;
+  s->rope = plain_rope(cfg->d_head);
   if (is_paged(*cfg)) {
     s->n_pages = (int)(cfg->kv_slots / cfg->page_slots);
     s->d_page_table = (int*)((char*)buffers->tables + tables_meta_bytes(*cfg) +
@@ -379,29 +463,63 @@ int sp_stage_create(const sp_config* cfg, const sp_layer_weights* layers, const 
     for (int i = 0; i < s->n_pages; ++i) s->free_pages[i] = s->n_pages - 1 - i;    // page 0 is handed out first
   }
   s->reqs.resize(cfg->max_requests);
+  s->use_graphs = !(cfg->flags & SP_FLAG_NO_GRAPHS);
+  *out = s;
+  return SP_OK;
+}
+
+int sp_stage_create(const sp_config* cfg, const sp_layer_weights* layers, const sp_buffers* buffers,
+                    sp_stream stream, sp_stage** out) {
+  int rc = check_config(cfg);
+  if (rc != SP_OK) return rc;
+  if (!layers || !buffers || !out) return SP_E_INVALID;
+  sp_sizes sz;
+  sp_stage_query_sizes(cfg, &sz);
+  sp_stage* s = nullptr;
+  if ((rc = make_stage(cfg, sz, buffers, &s)) != SP_OK) return rc;
+  for (int l = 0; l < cfg->n_layers; ++l) {
+    const sp_layer_weights& w = layers[l];
+    if (!w.wqkv || !w.wo || !w.wgu || !w.wd || !w.norm1 || !w.norm2 ||
+        (((uintptr_t)w.wqkv | (uintptr_t)w.wo | (uintptr_t)w.wgu | (uintptr_t)w.wd) & 15)) {
+      delete s;
+      return SP_E_INVALID;
+    }
+  }
+  s->W.assign(layers, layers + cfg->n_layers);
+  s->ws = carve(*cfg, (char*)buffers->workspace);
+  s->geom.scale_plane_bytes = scale_plane_bytes(*cfg);
+  if (is_fp4_kv(*cfg)) s->geom.scales = s->geom.kv + (size_t)cfg->n_layers * 2 * cfg->n_kv_heads * sz.kv_plane_bytes;
   // The MFMA kernels cover bf16 with d_head 128 and dimensions that fill their tiles.
   s->fast = cfg->dtype == SP_BF16 && !(cfg->flags & SP_FLAG_SIMPLE_KERNELS) && cfg->d_head == 128 &&
             cfg->d_model % 256 == 0 && cfg->d_ff % 256 == 0 &&
             (cfg->n_q_heads * cfg->d_head) % 256 == 0;
   s->f32 = cfg->dtype == SP_F32 && !(cfg->flags & SP_FLAG_SIMPLE_KERNELS);
-  {
-    int dev = 0, cus = 0;
-    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= SP_NOALLOC_MAX_DEVICES) { delete s; return SP_E_HIP; }
-    s->device = dev;
-    if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && cus > 0)
-      s->n_cu = cus;
-    s->o_resident = (size_t)cfg->n_layers * cfg->d_model * cfg->n_q_heads * cfg->d_head * 2 <= ((size_t)128 << 20);
-    if (!g_noalloc_scratch[dev]) {
-      // this device's copy of the static scratch array (the device is current here)
-      void* p = nullptr;
-      if (hipGetSymbolAddress(&p, HIP_SYMBOL(sp_noalloc_scratch)) != hipSuccess || !p) { delete s; return SP_E_HIP; }
-      g_noalloc_scratch[dev] = p;
-    }
-  }
-  s->use_graphs = !(cfg->flags & SP_FLAG_NO_GRAPHS);
+  s->o_resident = (size_t)cfg->n_layers * cfg->d_model * cfg->n_q_heads * cfg->d_head * 2 <= ((size_t)128 << 20);
   s->packed = (cfg->flags & SP_FLAG_PACKED_WEIGHTS) != 0;
   s->fp4 = (cfg->flags & SP_FLAG_FP4_WEIGHTS) != 0;
   if ((s->packed || s->fp4) && !s->fast) { delete s; return SP_E_UNSUPPORTED; }
+  hipError_t e = sp_launch_tables_clear(s->d_meta, s->d_tables, cfg->max_requests, (hipStream_t)stream);
+  if (e != hipSuccess) { delete s; return SP_E_HIP; }
+  *out = s;
+  return SP_OK;
+}
+
+int sp_latent_stage_create(const sp_config* cfg, const sp_latent* latent, const sp_buffers* buffers, sp_stream stream, sp_stage** out) {
+  int rc = check_latent(cfg, latent);
+  if (rc != SP_OK) return rc;
+  if (!buffers || !out) return SP_E_INVALID;
+  sp_sizes sz;
+  sp_latent_query_sizes(cfg, latent, &sz);
+  sp_stage* s = nullptr;
+  if ((rc = make_stage(cfg, sz, buffers, &s)) != SP_OK) return rc;
+  s->latent = true;
+  s->lat = {cfg->n_q_heads, latent->d_latent, latent->d_rope};
+  s->lat_scale = latent->scale;
+  if (latent->norms) s->lat_norms.assign(latent->norms, latent->norms + cfg->n_layers);
+  s->ws = carve_latent(*cfg, latent->d_latent, (char*)buffers->workspace);
+  s->geom.planes = cfg->n_layers;
+  s->rope = plain_rope(latent->d_rope);
+  s->fast = !(cfg->flags & SP_FLAG_SIMPLE_KERNELS) && cfg->d_model % 256 == 0;       // (the output head's kernels)
   hipError_t e = sp_launch_tables_clear(s->d_meta, s->d_tables, cfg->max_requests, (hipStream_t)stream);
   if (e != hipSuccess) { delete s; return SP_E_HIP; }
   *out = s;
@@ -737,6 +855,7 @@ static bool split_work(const sp_stage* s, AttnPlan& plan) {
 
 int sp_stage_forward(sp_stage* s, int32_t n_req, const int32_t* req_ids, const int32_t* first_node,
                      const int32_t* n_nodes, const void* x_in, void* x_out, sp_stream stream) {
+  if (s && s->latent) return SP_E_UNSUPPORTED;
   FwdBatch b;
   const int rc = call_rows(s, n_req, req_ids, first_node, n_nodes, b);
   if (rc != SP_OK) return rc;
@@ -757,9 +876,9 @@ int sp_stage_forward(sp_stage* s, int32_t n_req, const int32_t* req_ids, const i
   if (!split_work(s, plan)) return SP_E_CAPACITY;
 
   const size_t strideD = (size_t)M * d;
-  // Complete projections, and in float32 the joined one, rotate a few columns of a head at a time: heads that are normed, or held
-  // in groups of 32 columns, take the way over partial sums and a launch that has whole heads.
-  const bool whole_heads = kv4 || normed;
+  // Complete projections, and in float32 the joined one, rotate a few columns of a head at a time, all of them in halves: heads that
+  // are normed, rotated otherwise, or held in groups of 32 columns take the way over partial sums and a launch that has whole heads.
+  const bool whole_heads = kv4 || normed || s->rope.layout != SP_ROPE_HALVES || s->rope.dims != dh;
   const bool few = s->fast && !whole_heads && !s->fp4 && sp_few_takes(M, d, dq, F, s->packed, s->n_cu);
   // Activations between the products in fragment order, but few rows row-major where no product takes them by
   // direct-to-LDS loads; and in the many-row kernel beside row-major weights.  Complete projections: a k step is M pieces of
@@ -826,7 +945,7 @@ int sp_stage_forward(sp_stage* s, int32_t n_req, const int32_t* req_ids, const i
   auto rope_append = [&](int l, int S) -> hipError_t {
     ProfScope p(s, SP_K_ROPE_KV, st);
     if (whole_heads)
-      return sp_launch_append_parts(dt, w.part, S, (size_t)M * nqkv, w.rows, w.cs, normed ? s->norms[l].q : nullptr,
+      return sp_launch_append_parts(dt, w.part, S, (size_t)M * nqkv, w.rows, w.cs, s->rope, normed ? s->norms[l].q : nullptr,
                                     normed ? s->norms[l].k : nullptr, c.rms_eps, w.qbuf, s->geom, l, M, nq, nkv, dh, st);
     return sp_launch_rope_kv(dt, w.part, S, (size_t)M * nqkv, w.rows, w.cs, w.qbuf, s->geom, l, M, nq, nkv, dh, st);
   };
@@ -913,7 +1032,7 @@ int sp_stage_forward(sp_stage* s, int32_t n_req, const int32_t* req_ids, const i
 
   { ProfScope p(s, SP_K_NORM, st);
     SP_TRY(sp_launch_enter_norm(dt, x_in, plan, w.plan, s->d_meta, s->d_tables, w.rows, w.cs, dh,
-                                c.rope_theta, w.h, s->W[0].norm1, w.xn, frag, M, d, c.rms_eps, st)); }
+                                c.rope_theta, s->rope, w.h, s->W[0].norm1, w.xn, frag, M, d, c.rms_eps, st)); }
 
   // A shape of many launches that comes back replays its graph; one seen for the second time is captured.  Not while a
   // kernel kind is being timed (the events sit between the launches) and not inside a caller's capture.
@@ -993,6 +1112,7 @@ int sp_stage_forward(sp_stage* s, int32_t n_req, const int32_t* req_ids, const i
 // ---- a layer's attention piece by piece ---------------------------------------------------------
 int sp_stage_set_head_norms(sp_stage* s, const sp_head_norms* layers) {
   if (!s) return SP_E_INVALID;
+  if (s->latent) return SP_E_UNSUPPORTED;
   if (layers)
     for (int l = 0; l < s->cfg.n_layers; ++l) {
       if (!layers[l].q || !layers[l].k) return SP_E_INVALID;
@@ -1012,6 +1132,7 @@ int sp_stage_set_head_norms(sp_stage* s, const sp_head_norms* layers) {
 
 int sp_stage_append(sp_stage* s, int32_t layer, int32_t n_req, const int32_t* req_ids, const int32_t* first_node, const int32_t* n_nodes,
                     const void* qkv, void* q_out, sp_stream stream) {
+  if (s && s->latent) return SP_E_UNSUPPORTED;
   FwdBatch b;
   const int rc = call_rows(s, n_req, req_ids, first_node, n_nodes, b);
   if (rc != SP_OK) return rc;
@@ -1023,7 +1144,7 @@ int sp_stage_append(sp_stage* s, int32_t layer, int32_t n_req, const int32_t* re
   if (overlap(qkv, head_rows * (c.n_q_heads + 2 * c.n_kv_heads), q_out, head_rows * c.n_q_heads)) return SP_E_INVALID;
   const bool normed = !s->norms.empty();
   { ProfScope p(s, SP_K_ROPE_KV, (hipStream_t)stream);
-    const hipError_t e = sp_launch_append_rows(c.dtype, qkv, b, s->d_meta, s->d_tables, std::log2((double)c.rope_theta),
+    const hipError_t e = sp_launch_append_rows(c.dtype, qkv, b, s->d_meta, s->d_tables, std::log2((double)c.rope_theta), s->rope,
                                                normed ? s->norms[layer].q : nullptr, normed ? s->norms[layer].k : nullptr, c.rms_eps,
                                                q_out, s->geom, layer, c.n_q_heads, c.n_kv_heads, c.d_head, (hipStream_t)stream);
     if (e != hipSuccess) return hip_fail(s, e); }
@@ -1033,6 +1154,7 @@ int sp_stage_append(sp_stage* s, int32_t layer, int32_t n_req, const int32_t* re
 
 int sp_stage_attention(sp_stage* s, int32_t layer, int32_t n_req, const int32_t* req_ids, const int32_t* first_node,
                        const int32_t* n_nodes, const void* q, void* out, sp_stream stream) {
+  if (s && s->latent) return SP_E_UNSUPPORTED;
   FwdBatch b;
   const int rc = call_rows(s, n_req, req_ids, first_node, n_nodes, b);
   if (rc != SP_OK) return rc;
@@ -1064,8 +1186,9 @@ int sp_stage_attention(sp_stage* s, int32_t layer, int32_t n_req, const int32_t*
   return e == hipSuccess ? SP_OK : hip_fail(s, e);
 }
 
-static int check_slots(sp_stage* s, int32_t req, int32_t layer, int32_t first_slot, int32_t n, const void* k, const void* v) {
+static int check_slots(sp_stage* s, bool latent, int32_t req, int32_t layer, int32_t first_slot, int32_t n, const void* k, const void* v) {
   if (!s) return SP_E_INVALID;
+  if (s->latent != latent) return SP_E_UNSUPPORTED;
   HostReq* r = get_req(s, req);
   if (!r) return SP_E_BAD_REQ;
   if (r->pending) return SP_E_PENDING;
@@ -1076,7 +1199,7 @@ static int check_slots(sp_stage* s, int32_t req, int32_t layer, int32_t first_sl
 }
 
 int sp_kv_store(sp_stage* s, int32_t req, int32_t layer, int32_t first_slot, int32_t n, const void* k, const void* v, sp_stream stream) {
-  const int rc = check_slots(s, req, layer, first_slot, n, k, v);
+  const int rc = check_slots(s, false, req, layer, first_slot, n, k, v);
   if (rc != SP_OK || n == 0) return rc;
   const hipError_t e = sp_launch_kv_store(s->cfg.dtype, s->geom, req, s->reqs[req].base, layer, first_slot, n, k, v, s->cfg.n_kv_heads,
                                           s->cfg.d_head, (hipStream_t)stream);
@@ -1084,13 +1207,167 @@ int sp_kv_store(sp_stage* s, int32_t req, int32_t layer, int32_t first_slot, int
 }
 
 int sp_kv_load(sp_stage* s, int32_t req, int32_t layer, int32_t first_slot, int32_t n, void* k, void* v, sp_stream stream) {
-  const int rc = check_slots(s, req, layer, first_slot, n, k, v);
+  const int rc = check_slots(s, false, req, layer, first_slot, n, k, v);
   if (rc != SP_OK || n == 0) return rc;
   const size_t bytes = (size_t)n * s->cfg.n_kv_heads * s->cfg.d_head * elt_bytes(s->cfg.dtype);
   if (overlap(k, bytes, v, bytes)) return SP_E_INVALID;
   const hipError_t e = sp_launch_kv_load(s->cfg.dtype, s->geom, req, s->reqs[req].base, layer, first_slot, n, k, v, s->cfg.n_kv_heads,
                                          s->cfg.d_head, (hipStream_t)stream);
   return e == hipSuccess ? SP_OK : hip_fail(s, e);
+}
+
+// ---- rotary positions -----------------------------------------------------------------------------
+int sp_rope_frequencies(int32_t dims, double theta, int32_t scaling, double factor, double original, double first, double second,
+                        double* freq_out) {
+  if (!freq_out || dims < 8 || dims % 8 || dims > 2 * SP_ROPE_MAX_PAIRS || !(theta > 1.) || !std::isfinite(theta)) return SP_E_INVALID;
+  if (scaling < SP_ROPE_PLAIN || scaling > SP_ROPE_RAMP) return SP_E_INVALID;
+  if (scaling != SP_ROPE_PLAIN && (!(factor >= 1.) || !std::isfinite(factor))) return SP_E_INVALID;
+  if (scaling == SP_ROPE_BANDS || scaling == SP_ROPE_RAMP) {
+    if (!(original > 0.) || !std::isfinite(original) || !(first > 0.) || !(second > 0.) || !std::isfinite(first) || !std::isfinite(second)) return SP_E_INVALID;
+    if (scaling == SP_ROPE_BANDS ? !(first < second) : !(first > second)) return SP_E_INVALID;
+  }
+  rope_frequencies(dims, theta, scaling, factor, original, first, second, freq_out);
+  return SP_OK;
+}
+
+static int check_rope(const sp_rope* r, int cols) {
+  if (!r || (r->layout != SP_ROPE_HALVES && r->layout != SP_ROPE_INTERLEAVED)) return SP_E_INVALID;
+  if (r->dims < 8 || r->dims % 8 || r->dims > cols || r->dims > 2 * SP_ROPE_MAX_PAIRS || !std::isfinite(r->gain)) return SP_E_INVALID;
+  for (int t = 0; t < r->dims / 2; ++t) if (!std::isfinite(r->freq[t])) return SP_E_INVALID;
+  return SP_OK;
+}
+
+int sp_rotate(const sp_rope* rope, int32_t dtype, int32_t inverse, const void* x, int64_t x_row, int64_t x_head, int32_t n_rows, int32_t n_heads,
+              int32_t d_head, const int32_t* positions, void* out, int64_t out_row, int64_t out_head, sp_stream stream) {
+  if (n_rows < 0 || n_heads < 1 || d_head < 8 || (dtype != SP_F32 && dtype != SP_BF16) || (inverse != 0 && inverse != 1)) return SP_E_INVALID;
+  if (d_head % 8 || d_head > 2 * SP_ROPE_MAX_PAIRS) return SP_E_UNSUPPORTED;
+  const int rc = check_rope(rope, d_head);
+  if (rc != SP_OK) return rc;
+  if (n_rows == 0) return SP_OK;
+  if (!x || !out || !positions || (((uintptr_t)x | (uintptr_t)out) & 15) || ((uintptr_t)positions & 3)) return SP_E_INVALID;
+  const int64_t in = strided_extent(n_rows, x_row, n_heads, x_head, d_head, false);
+  const int64_t to = strided_extent(n_rows, out_row, n_heads, out_head, d_head, true);
+  if (in < 0 || to < 0) return SP_E_UNSUPPORTED;
+  const size_t eb = elt_bytes(dtype);
+  const bool in_place = x == out && x_row == out_row && x_head == out_head;
+  if (!in_place && overlap(x, in * eb, out, to * eb)) return SP_E_INVALID;
+  if (overlap(positions, (size_t)n_rows * 4, out, to * eb)) return SP_E_INVALID;
+  RotateArgs a;
+  a.x = x; a.out = out;
+  a.x_row = x_row; a.x_head = x_head; a.out_row = out_row; a.out_head = out_head;
+  a.pos = positions;
+  a.n_rows = n_rows; a.n_heads = n_heads; a.d_head = d_head; a.dims = rope->dims; a.layout = rope->layout;
+  a.gain = rope->gain; a.sign = inverse ? -1.f : 1.f;
+  static_assert(sizeof(a.freq) == sizeof(rope->freq), "frequencies");
+  std::memcpy(a.freq, rope->freq, sizeof(double) * (rope->dims / 2));
+  return sp_launch_rotate(dtype, a, (hipStream_t)stream) == hipSuccess ? SP_OK : SP_E_HIP;
+}
+
+int sp_stage_set_rope(sp_stage* s, const sp_rope* rope) {
+  if (!s) return SP_E_INVALID;
+  const int cols = s->latent ? s->lat.d_rope : s->cfg.d_head;
+  StageRope next = plain_rope(cols);
+  if (rope) {
+    const int rc = check_rope(rope, cols);
+    if (rc != SP_OK) return rc;
+    if (s->geom.scales && rope->layout == SP_ROPE_HALVES && rope->dims % 64 && rope->dims != cols) return SP_E_UNSUPPORTED;
+    next.on = 1;
+    next.layout = rope->layout; next.dims = rope->dims; next.gain = rope->gain;
+    std::memcpy(next.freq, rope->freq, sizeof(double) * (rope->dims / 2));
+  }
+  // what was captured may launch other kernels than calls from now on
+  if (!s->graphs.empty()) {
+    const hipError_t e = hipDeviceSynchronize();
+    if (e != hipSuccess) return hip_fail(s, e);
+  }
+  s->rope = next;
+  for (auto& g : s->graphs) if (g.exec) (void)hipGraphExecDestroy(g.exec);
+  s->graphs.clear();
+  return SP_OK;
+}
+
+// ---- a cache of latent vectors ----------------------------------------------------------------------
+int sp_latent_store(sp_stage* s, int32_t req, int32_t layer, int32_t first_slot, int32_t n, const void* rows, sp_stream stream) {
+  const int rc = check_slots(s, true, req, layer, first_slot, n, rows, rows);
+  if (rc != SP_OK || n == 0) return rc;
+  const hipError_t e = sp_launch_latent_rows(true, s->geom, req, s->reqs[req].base, layer, first_slot, n, const_cast<void*>(rows), (hipStream_t)stream);
+  return e == hipSuccess ? SP_OK : hip_fail(s, e);
+}
+
+int sp_latent_load(sp_stage* s, int32_t req, int32_t layer, int32_t first_slot, int32_t n, void* rows, sp_stream stream) {
+  const int rc = check_slots(s, true, req, layer, first_slot, n, rows, rows);
+  if (rc != SP_OK || n == 0) return rc;
+  const hipError_t e = sp_launch_latent_rows(false, s->geom, req, s->reqs[req].base, layer, first_slot, n, rows, (hipStream_t)stream);
+  return e == hipSuccess ? SP_OK : hip_fail(s, e);
+}
+
+int sp_latent_append(sp_stage* s, int32_t layer, int32_t n_req, const int32_t* req_ids, const int32_t* first_node, const int32_t* n_nodes,
+                     const void* q, int64_t q_row, int64_t q_head, const void* kv, int64_t kv_row, void* q_out, int64_t out_row,
+                     int64_t out_head, sp_stream stream) {
+  if (s && !s->latent) return SP_E_UNSUPPORTED;
+  FwdBatch b;
+  const int rc = call_rows(s, n_req, req_ids, first_node, n_nodes, b);
+  if (rc != SP_OK) return rc;
+  if (layer < 0 || layer >= s->cfg.n_layers) return SP_E_INVALID;
+  if (b.n_rows == 0) return SP_OK;
+  if (!q || !kv || !q_out || (((uintptr_t)q | (uintptr_t)kv | (uintptr_t)q_out) & 15)) return SP_E_INVALID;
+  const LatentDims& d = s->lat;
+  const int64_t in = strided_extent(b.n_rows, q_row, d.n_heads, q_head, d.d_rope, false);
+  const int64_t rows = strided_extent(b.n_rows, kv_row, 1, 0, d.d_latent + d.d_rope, false);
+  const int64_t to = strided_extent(b.n_rows, out_row, d.n_heads, out_head, d.d_rope, true);
+  if (in < 0 || rows < 0 || to < 0) return SP_E_UNSUPPORTED;
+  const bool in_place = q == q_out && q_row == out_row && q_head == out_head;
+  if ((!in_place && overlap(q, in * 2, q_out, to * 2)) || overlap(kv, rows * 2, q_out, to * 2)) return SP_E_INVALID;
+  LatentAppendArgs a;
+  a.q = (const bf16_t*)q; a.q_row = q_row; a.q_head = q_head;
+  a.kv = (const bf16_t*)kv; a.kv_row = kv_row;
+  a.q_out = (bf16_t*)q_out; a.out_row = out_row; a.out_head = out_head;
+  a.gain = s->lat_norms.empty() ? nullptr : (const bf16_t*)s->lat_norms[layer];
+  a.eps = s->cfg.rms_eps;
+  a.log2_theta = std::log2((double)s->cfg.rope_theta);
+  a.rope = s->rope;
+  a.meta = s->d_meta; a.tables = s->d_tables;
+  a.g = s->geom;
+  a.layer = layer;
+  a.d = d;
+  { ProfScope p(s, SP_K_ROPE_KV, (hipStream_t)stream);
+    const hipError_t e = sp_launch_latent_append(a, b, (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(s, e); }
+  if (layer == s->cfg.n_layers - 1) mark_forwarded(s, b);
+  return SP_OK;
+}
+
+int sp_latent_attention(sp_stage* s, int32_t layer, int32_t n_req, const int32_t* req_ids, const int32_t* first_node, const int32_t* n_nodes,
+                        const void* q, void* out, sp_stream stream) {
+  if (s && !s->latent) return SP_E_UNSUPPORTED;
+  FwdBatch b;
+  const int rc = call_rows(s, n_req, req_ids, first_node, n_nodes, b);
+  if (rc != SP_OK) return rc;
+  if (layer < 0 || layer >= s->cfg.n_layers) return SP_E_INVALID;
+  if (b.n_rows == 0) return SP_OK;
+  if (!q || !out || (((uintptr_t)q | (uintptr_t)out) & 15)) return SP_E_INVALID;
+  const LatentDims& d = s->lat;
+  const size_t heads = (size_t)b.n_rows * d.n_heads;
+  if (overlap(q, heads * (d.d_latent + d.d_rope) * 2, out, heads * d.d_latent * 2)) return SP_E_INVALID;
+  AttnPlan plan;
+  plan_segments(s, b, nullptr, plan);
+  const LatentAttnArgs a = {(const bf16_t*)q, (bf16_t*)out, s->d_tables, s->geom, layer, d, s->lat_scale, s->ws.attn_part};
+  ProfScope p(s, SP_K_ATTENTION, (hipStream_t)stream);
+  const hipError_t e = sp_launch_latent_attn_simple(a, plan, b.n_rows, (hipStream_t)stream);
+  return e == hipSuccess ? SP_OK : hip_fail(s, e);
+}
+
+int sp_head_product(const void* x, int64_t x_row, int64_t x_head, int32_t m, int32_t heads, const void* w, int32_t n, int32_t k, void* out,
+                    int64_t out_row, int64_t out_head, sp_stream stream) {
+  if (m < 0 || heads < 1 || n < 1 || k < 1) return SP_E_INVALID;
+  if (n % 16 || k % 32 || n > SP_HEAD_PRODUCT_MAX || k > SP_HEAD_PRODUCT_MAX || heads > SP_HEAD_PRODUCT_MAX) return SP_E_UNSUPPORTED;
+  if (m == 0) return SP_OK;
+  if (!x || !w || !out || (((uintptr_t)x | (uintptr_t)w | (uintptr_t)out) & 15)) return SP_E_INVALID;
+  const int64_t in = strided_extent(m, x_row, heads, x_head, k, false), to = strided_extent(m, out_row, heads, out_head, n, true);
+  if (in < 0 || to < 0) return SP_E_UNSUPPORTED;
+  if (overlap(x, in * 2, out, to * 2) || overlap(w, (size_t)heads * n * k * 2, out, to * 2)) return SP_E_INVALID;
+  const HeadProductArgs a = {(const bf16_t*)x, (const bf16_t*)w, (bf16_t*)out, x_row, x_head, out_row, out_head, m, heads, n, k};
+  return sp_launch_head_product(a, (hipStream_t)stream) == hipSuccess ? SP_OK : SP_E_HIP;
 }
 
 int sp_tree_prune_batch(sp_stage* s, int32_t n, const int32_t* req_ids, const int32_t* modes, const int32_t* nodes,
@@ -1342,8 +1619,8 @@ static int verify_head_on(sp_stage* s, const HeadScratch& w, const sp_head_weigh
     rows_of.seg_row0[i] = b.row0[i]; rows_of.seg_rows[i] = b.n[i]; rows_of.seg_req[i] = b.req[i];
     rows_of.seg_first[i] = b.first[i];
   }
-  e = sp_launch_enter_norm(c.dtype, x, rows_of, nullptr, s->d_meta, s->d_tables, w.rows, w.cs, c.d_head, c.rope_theta,
-                           w.h, head->norm, w.xn, head_rows_frag(s, V), M, d, c.rms_eps, st);
+  e = sp_launch_enter_norm(c.dtype, x, rows_of, nullptr, s->d_meta, s->d_tables, w.rows, w.cs, s->latent ? 64 : c.d_head, c.rope_theta,
+                           plain_rope(64), w.h, head->norm, w.xn, head_rows_frag(s, V), M, d, c.rms_eps, st);
   if (e != hipSuccess) return hip_fail(s, e);
   ProfScope p(s, SP_K_VERIFY_HEAD, st);
   if (head_on_mfma(s, V)) {
@@ -1382,7 +1659,7 @@ int sp_stage_verify_head_noalloc(sp_stage* s, const sp_head_weights* head, int32
   auto take = [&](size_t bytes) { char* p = base + off; off += align_up(bytes); return (void*)p; };
   HeadScratch w;
   w.rows = (RowInfo*)take(R * sizeof(RowInfo));
-  w.cs = (float*)take(R * c.d_head * sizeof(float));
+  w.cs = (float*)take(R * (s->latent ? 64 : c.d_head) * sizeof(float));
   w.h = (float*)take(R * c.d_model * sizeof(float));
   w.xn = take(R * c.d_model * (size_t)elt_bytes(c.dtype));
   if (off + 256 > SP_NOALLOC_SCRATCH_BYTES) return SP_E_CAPACITY;      // d_model too large for the array

@@ -27,14 +27,14 @@ __device__ __forceinline__ void store4(bf16_t* p, const float (&v)[4]) {
   *reinterpret_cast<uint2*>(p) = uint2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
 }
 
-// Columns t .. t+3 and half + t .. + 3 of a head into slot `slot` of a plane of the cache (all lanes of the wave that have a head
-// come here together: the groups' maxima are taken across lanes).
+// Columns ca .. ca+3 and cb .. cb+3 of a head into slot `slot` of a plane of the cache (all lanes of the wave that have a head
+// come here together: the groups' maxima are taken across lanes; eight lanes have 32 columns in a row twice).
 template <typename T, bool FP4>
-__device__ __forceinline__ void put_row(const KvGeom& g, size_t plane, size_t slot, int half, int t, const float (&a)[4], const float (&b)[4]) {
+__device__ __forceinline__ void put_row(const KvGeom& g, size_t plane, size_t slot, int ca, int cb, const float (&a)[4], const float (&b)[4]) {
   char* row = g.kv + plane * g.plane_bytes + slot * g.row_bytes;
   if constexpr (!FP4) {
-    store4(reinterpret_cast<T*>(row) + t, a);
-    store4(reinterpret_cast<T*>(row) + half + t, b);
+    store4(reinterpret_cast<T*>(row) + ca, a);
+    store4(reinterpret_cast<T*>(row) + cb, b);
   } else {
     // four values of eight lanes are a group, in either half
     float ma = 0.f, mb = 0.f;
@@ -43,12 +43,12 @@ __device__ __forceinline__ void put_row(const KvGeom& g, size_t plane, size_t sl
 #pragma unroll
     for (int o = 1; o < 8; o <<= 1) { ma = fmaxf(ma, __shfl_xor(ma, o, 64)); mb = fmaxf(mb, __shfl_xor(mb, o, 64)); }
     const uint32_t ba = fp4_biased(ma), bb = fp4_biased(mb);
-    reinterpret_cast<unsigned short*>(row)[t >> 2] = (unsigned short)fp4_codes4(a, fp4_scale(ba));
-    reinterpret_cast<unsigned short*>(row)[(half + t) >> 2] = (unsigned short)fp4_codes4(b, fp4_scale(bb));
-    if ((t & 31) == 0) {
+    reinterpret_cast<unsigned short*>(row)[ca >> 2] = (unsigned short)fp4_codes4(a, fp4_scale(ba));
+    reinterpret_cast<unsigned short*>(row)[cb >> 2] = (unsigned short)fp4_codes4(b, fp4_scale(bb));
+    if ((ca & 31) == 0) {
       unsigned char* sc = reinterpret_cast<unsigned char*>(g.scales + plane * g.scale_plane_bytes + slot * 4);
-      sc[t / FP4_GROUP] = (unsigned char)ba;
-      sc[(half + t) / FP4_GROUP] = (unsigned char)bb;
+      sc[ca / FP4_GROUP] = (unsigned char)ba;
+      sc[cb / FP4_GROUP] = (unsigned char)bb;
     }
   }
 }
@@ -68,6 +68,7 @@ struct AppendArgs {
   void* q;                  // [rows][n_q * d_head]
   KvGeom g;
   int layer, n_q, n_kv, d_head;
+  StageRope rope;           // (PART: its layout and dims, the angles are in cs)
 };
 
 // grid: (rows, ceil(heads / (256 / (d_head / 8)))).  T: storage of the rows, and of the cache unless FP4.
@@ -77,33 +78,38 @@ __global__ void __launch_bounds__(256) k_head_append(AppendArgs a, FwdBatch b) {
   const int half = a.d_head >> 1, tph = half >> 2, row = blockIdx.x;
   const int head = blockIdx.y * (256 / tph) + threadIdx.x / tph;
   const int t = (threadIdx.x % tph) * 4;
+  // The lane's columns: in halves four pairs of the rotated columns, or, behind their lanes, columns that pass; interleaved two
+  // pairs and two pairs.
+  const int pairs = a.rope.dims >> 1;
+  const bool halves = a.rope.layout == 0, passes = halves && t >= pairs;
+  const int ca = passes ? a.rope.dims + t - pairs : t, cb = !halves ? half + t : passes ? a.rope.dims + half - pairs + t - pairs : pairs + t;
   const int heads = a.n_q + 2 * a.n_kv;
   const bool on = head < heads, rotated = head < a.n_q + a.n_kv;
 
   // the row's values are asked for before the position is known
   float u[4] = {0.f, 0.f, 0.f, 0.f}, v[4] = {0.f, 0.f, 0.f, 0.f};
   if (on) {
-    const size_t at = ((size_t)row * heads + head) * a.d_head + t;
+    const size_t at = ((size_t)row * heads + head) * a.d_head;
     if constexpr (PART) {
       const float* p = reinterpret_cast<const float*>(a.x) + at;
       for (int s = 0; s < a.S; ++s) {
         float du[4], dv[4];
-        load4(p + (size_t)s * a.part_stride, du);
-        load4(p + (size_t)s * a.part_stride + half, dv);
+        load4(p + (size_t)s * a.part_stride + ca, du);
+        load4(p + (size_t)s * a.part_stride + cb, dv);
 #pragma unroll
         for (int i = 0; i < 4; ++i) { u[i] += du[i]; v[i] += dv[i]; }
       }
     } else {
-      load4(reinterpret_cast<const T*>(a.x) + at, u);
-      load4(reinterpret_cast<const T*>(a.x) + at + half, v);
+      load4(reinterpret_cast<const T*>(a.x) + at + ca, u);
+      load4(reinterpret_cast<const T*>(a.x) + at + cb, v);
     }
   }
   const bool normed = a.gain_q != nullptr && rotated;
   float gu[4] = {1.f, 1.f, 1.f, 1.f}, gv[4] = {1.f, 1.f, 1.f, 1.f};
   if (normed) {
     const T* gain = reinterpret_cast<const T*>(head < a.n_q ? a.gain_q : a.gain_k);
-    load4(gain + t, gu);
-    load4(gain + half + t, gv);
+    load4(gain + ca, gu);
+    load4(gain + cb, gv);
   }
 
   size_t slot;
@@ -127,10 +133,11 @@ __global__ void __launch_bounds__(256) k_head_append(AppendArgs a, FwdBatch b) {
     // The angle in double precision, whole turns taken off there: positions of tens of thousands keep full float accuracy.
     if ((int)threadIdx.x < half) {
       const double pos = (double)(m.P + depth);
-      const double turns = pos * exp2(-(2.0 * (double)threadIdx.x / (double)a.d_head) * a.log2_theta) * 0.15915494309189535;
+      const double turns = pos * (a.rope.on ? a.rope.freq[threadIdx.x] : exp2(-(2.0 * (double)threadIdx.x / (double)a.d_head) * a.log2_theta)) * 0.15915494309189535;
       const float ang = (float)((turns - rint(turns)) * 6.283185307179586);
-      s_cs[threadIdx.x] = cosf(ang);
-      s_cs[half + threadIdx.x] = sinf(ang);
+      const bool turns_at_all = (int)threadIdx.x < pairs;
+      s_cs[threadIdx.x] = turns_at_all ? cosf(ang) * a.rope.gain : 1.f;
+      s_cs[half + threadIdx.x] = turns_at_all ? sinf(ang) * a.rope.gain : 0.f;
     }
     __syncthreads();
     cs = s_cs;
@@ -145,7 +152,7 @@ __global__ void __launch_bounds__(256) k_head_append(AppendArgs a, FwdBatch b) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) { u[i] *= r * gu[i]; v[i] *= r * gv[i]; }
   }
-  if (rotated) {
+  if (rotated && halves && !passes) {
     float co[4], si[4];
     load4(cs + t, co);
     load4(cs + half + t, si);
@@ -155,16 +162,26 @@ __global__ void __launch_bounds__(256) k_head_append(AppendArgs a, FwdBatch b) {
       u[i] = x * co[i] - y * si[i];
       v[i] = y * co[i] + x * si[i];
     }
+  } else if (rotated && !halves) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float ua = u[2 * i], ub = u[2 * i + 1], va = v[2 * i], vb = v[2 * i + 1];
+      const float uc = cs[ca / 2 + i], us = cs[half + ca / 2 + i], vc = cs[cb / 2 + i], vs = cs[half + cb / 2 + i];
+      u[2 * i] = ua * uc - ub * us;
+      u[2 * i + 1] = ub * uc + ua * us;
+      v[2 * i] = va * vc - vb * vs;
+      v[2 * i + 1] = vb * vc + va * vs;
+    }
   }
   if (!on) return;
   if (head < a.n_q) {
     T* dst = reinterpret_cast<T*>(a.q) + ((size_t)row * a.n_q + head) * a.d_head;
-    store4(dst + t, u);
-    store4(dst + half + t, v);
+    store4(dst + ca, u);
+    store4(dst + cb, v);
   } else {
     const bool is_v = head >= a.n_q + a.n_kv;
     const size_t plane = (size_t)(a.layer * 2 + (is_v ? 1 : 0)) * a.n_kv + (head - a.n_q - (is_v ? a.n_kv : 0));
-    put_row<T, FP4>(a.g, plane, slot, half, t, u, v);
+    put_row<T, FP4>(a.g, plane, slot, ca, cb, u, v);
   }
 }
 
@@ -184,7 +201,7 @@ __global__ void __launch_bounds__(256) k_head_rows(KvGeom g, int req, long long 
   if constexpr (STORE) {
     load4(p + t, a);
     load4(p + half + t, b);
-    put_row<T, FP4>(g, plane, slot, half, t, a, b);
+    put_row<T, FP4>(g, plane, slot, t, half + t, a, b);
   } else {
     const char* src = g.kv + plane * g.plane_bytes + slot * g.row_bytes;
     if constexpr (FP4) {
@@ -215,17 +232,17 @@ static hipError_t go_append(int dtype, const AppendArgs& a, const FwdBatch& b, i
 
 static_assert(sizeof(AppendArgs) + sizeof(FwdBatch) <= 4096, "kernel arguments");
 hipError_t sp_launch_append_parts(int dtype, const float* part, int S, size_t part_stride, const RowInfo* rows, const float* cs,
-                                  const void* gain_q, const void* gain_k, float eps, void* qbuf, KvGeom g, int layer, int M,
-                                  int n_q, int n_kv, int d_head, hipStream_t st) {
-  AppendArgs a{part, S, part_stride, rows, cs, nullptr, nullptr, 0., gain_q, gain_k, eps, qbuf, g, layer, n_q, n_kv, d_head};
+                                  const StageRope& rope, const void* gain_q, const void* gain_k, float eps, void* qbuf, KvGeom g,
+                                  int layer, int M, int n_q, int n_kv, int d_head, hipStream_t st) {
+  AppendArgs a{part, S, part_stride, rows, cs, nullptr, nullptr, 0., gain_q, gain_k, eps, qbuf, g, layer, n_q, n_kv, d_head, rope};
   FwdBatch none;
   none.n_req = 0; none.n_rows = 0;
   return go_append<true>(dtype, a, none, M, st);
 }
 hipError_t sp_launch_append_rows(int dtype, const void* x, const FwdBatch& b, const ReqMeta* meta, const ReqTables* tables,
-                                 double log2_theta, const void* gain_q, const void* gain_k, float eps, void* q, KvGeom g, int layer,
-                                 int n_q, int n_kv, int d_head, hipStream_t st) {
-  AppendArgs a{x, 1, 0, nullptr, nullptr, meta, tables, log2_theta, gain_q, gain_k, eps, q, g, layer, n_q, n_kv, d_head};
+                                 double log2_theta, const StageRope& rope, const void* gain_q, const void* gain_k, float eps, void* q,
+                                 KvGeom g, int layer, int n_q, int n_kv, int d_head, hipStream_t st) {
+  AppendArgs a{x, 1, 0, nullptr, nullptr, meta, tables, log2_theta, gain_q, gain_k, eps, q, g, layer, n_q, n_kv, d_head, rope};
   return go_append<false>(dtype, a, b, b.n_rows, st);
 }
 

@@ -2,6 +2,7 @@
 // the launch status; none synchronises.
 #pragma once
 #include "sp_device.h"
+#include "sp_rope.h"
 
 struct KvGeom {
   char* kv;              // slab
@@ -9,6 +10,7 @@ struct KvGeom {
   int row_bytes;         // d_head * element size
   int n_layers;
   int n_kv_heads;
+  int planes;            // of the slab: layers * 2 * KV heads, or the layers of a latent cache
   // Paged storage (SpecPipe-DB keeps its cache in pages, Sec. 4 "Implementation"): request r's
   // logical slot s lives in physical slot page_table[r * pt_stride + (s >> pg_shift)] << pg_shift
   // | (s & mask).  Null: a request owns the contiguous range that starts at its base slot.
@@ -77,8 +79,8 @@ hipError_t sp_launch_kv_compact(const ReqMeta* meta, const ReqTables* tables, co
 // whole plan is also stored there for the attention kernels of the call.
 hipError_t sp_launch_enter_norm(int dtype, const void* x, const AttnPlan& plan, AttnPlan* plan_dev /*nullable*/,
                                 const ReqMeta* meta, const ReqTables* tables, RowInfo* rows, float* cs, int d_head,
-                                float theta, float* h, const void* gain, void* xn, bool frag, int M, int d, float eps,
-                                hipStream_t st);
+                                float theta, const StageRope& rope, float* h, const void* gain, void* xn, bool frag, int M, int d,
+                                float eps, hipStream_t st);
 
 // h += sum_s part[s]; xn = rmsnorm(h) * gain
 hipError_t sp_launch_add_norm(int dtype, float* h, const float* part, int S, size_t part_stride,
@@ -177,11 +179,11 @@ hipError_t sp_launch_attn_fp4(const bf16_t* q, const ReqTables* tables, KvGeom g
 // Head norms (gains nullable: none), rotation and cache append (sp_heads.hip) of QKV rows; into whichever cache g describes.
 // _parts: float32 sums of slices, with the forward call's row descriptors; _rows: rows in the storage type
 hipError_t sp_launch_append_parts(int dtype, const float* part, int S, size_t part_stride, const RowInfo* rows, const float* cs,
-                                  const void* gain_q, const void* gain_k, float eps, void* qbuf, KvGeom g, int layer, int M,
-                                  int n_q, int n_kv, int d_head, hipStream_t st);
+                                  const StageRope& rope, const void* gain_q, const void* gain_k, float eps, void* qbuf, KvGeom g,
+                                  int layer, int M, int n_q, int n_kv, int d_head, hipStream_t st);
 hipError_t sp_launch_append_rows(int dtype, const void* x, const FwdBatch& b, const ReqMeta* meta, const ReqTables* tables,
-                                 double log2_theta, const void* gain_q, const void* gain_k, float eps, void* q, KvGeom g, int layer,
-                                 int n_q, int n_kv, int d_head, hipStream_t st);
+                                 double log2_theta, const StageRope& rope, const void* gain_q, const void* gain_k, float eps, void* q,
+                                 KvGeom g, int layer, int n_q, int n_kv, int d_head, hipStream_t st);
 // K and V rows [n][n_kv][d_head] of logical slots first .. first + n - 1 into the cache, and out of it
 hipError_t sp_launch_kv_store(int dtype, KvGeom g, int req, long long base, int layer, int first, int n, const void* k, const void* v,
                               int n_kv, int d_head, hipStream_t st);
@@ -202,3 +204,61 @@ hipError_t sp_launch_fp4_product(const bf16_t* X, const void* W, bool gated, bf1
 // row descriptors of a call's rows, and its plan, to device memory
 hipError_t sp_launch_call_rows(const AttnPlan& plan, AttnPlan* plan_dev, const ReqMeta* meta, const ReqTables* tables, RowInfo* rows,
                                int M, hipStream_t st);
+
+// ---- rotary positions of rows of heads (sp_rope.hip) --------------------------------
+// rows [n_rows][n_heads] of d_head columns, row and head strides in elements (multiples of 8); out may be x in place
+struct RotateArgs {
+  const void* x;
+  void* out;
+  long long x_row, x_head, out_row, out_head;
+  const int* pos;                  // [n_rows]
+  int n_rows, n_heads, d_head, dims, layout;
+  float gain, sign;                // sign -1: back
+  double freq[2 * SP_ROPE_PAIRS];
+};
+hipError_t sp_launch_rotate(int dtype, const RotateArgs& a, hipStream_t st);
+
+// ---- latent cache: one row of d_latent + d_rope bf16 values a token and layer ---------
+struct LatentDims { int n_heads, d_latent, d_rope; };
+struct LatentAppendArgs {
+  const bf16_t* q;                 // the query heads' rotated parts, [rows][n_heads] of d_rope columns
+  long long q_row, q_head;
+  const bf16_t* kv;                // [rows] of d_latent + d_rope columns
+  long long kv_row;
+  bf16_t* q_out;
+  long long out_row, out_head;
+  const bf16_t* gain;              // [d_latent], null: no norm
+  float eps;
+  double log2_theta;
+  StageRope rope;
+  const ReqMeta* meta;
+  const ReqTables* tables;
+  KvGeom g;
+  int layer;
+  LatentDims d;
+};
+hipError_t sp_launch_latent_append(const LatentAppendArgs& a, const FwdBatch& b, hipStream_t st);
+// rows of logical slots first .. first + n - 1 into the cache (store) or out of it
+hipError_t sp_launch_latent_rows(bool store, KvGeom g, int req, long long base, int layer, int first, int n, void* rows, hipStream_t st);
+// Tree attention: out[row][head][0 .. d_latent) = softmax(scale * q . cache row + tree mask) . cache row's latent columns
+struct LatentAttnArgs {
+  const bf16_t* q;                 // [M][n_heads][d_latent + d_rope]
+  bf16_t* out;                     // [M][n_heads][d_latent]
+  const ReqTables* tables;
+  KvGeom g;
+  int layer;
+  LatentDims d;
+  float scale;
+  float* part;                     // partial results of ranges that are cut
+};
+hipError_t sp_launch_latent_attn_simple(const LatentAttnArgs& a, const AttnPlan& plan, int M, hipStream_t st);
+
+// ---- products head by head (sp_head_product.hip) --------------------------------------
+struct HeadProductArgs {
+  const bf16_t* x;                 // [m][heads] of k columns
+  const bf16_t* w;                 // [heads][n][k]
+  bf16_t* out;                     // [m][heads] of n columns
+  long long x_row, x_head, out_row, out_head;
+  int m, heads, n, k;
+};
+hipError_t sp_launch_head_product(const HeadProductArgs& a, hipStream_t st);

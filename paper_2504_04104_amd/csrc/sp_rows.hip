@@ -69,13 +69,16 @@ __host__ __device__ inline int norm_blocks(int M, bool frag) { return norm_group
 struct NoPlan { int unused; };
 template <bool FIRST> struct PlanArg { typedef NoPlan type; };
 template <> struct PlanArg<true> { typedef AttnPlan type; };
+template <bool FIRST> struct RopeParam { typedef NoPlan type; };
+template <> struct RopeParam<true> { typedef StageRope type; };
+static_assert(sizeof(AttnPlan) + sizeof(StageRope) + 160 <= 4096, "kernel arguments");
 
 template <typename T, bool FIRST>
 __global__ void __launch_bounds__(1024) k_add_norm(float* h, const float* part, int S, size_t part_stride,
                                                     const T* gain, T* xn, int M, int d, float eps, const T* x,
                                                     typename PlanArg<FIRST>::type b, AttnPlan* plan_dev,
                                                     const ReqMeta* meta, const ReqTables* tables, RowInfo* rows,
-                                                    float* cs, int d_head, float theta, bool frag) {
+                                                    float* cs, int d_head, float theta, bool frag, typename RopeParam<FIRST>::type rope) {
   __shared__ float s_red[16];
   const int row_blocks = norm_blocks(M, frag);
   const int row = norm_grouped(M, frag) ? (((blockIdx.x >> 6) * 8 + (blockIdx.x & 7)) * 8 + ((blockIdx.x >> 3) & 7)) : blockIdx.x;
@@ -95,10 +98,15 @@ __global__ void __launch_bounds__(1024) k_add_norm(float* h, const float* part, 
           ri.base = m.base; ri.req = req; ri.node = node; ri.pos = pos; ri.P = m.P; ri.T = m.T;
           rows[r] = ri;
         }
-        const double inv_freq = exp2(-(2.0 * (double)tt / (double)d_head) * log2((double)theta));
-        const double ang = (double)pos * inv_freq;
-        cs[(size_t)r * d_head + tt] = (float)cos(ang);
-        cs[(size_t)r * d_head + half + tt] = (float)sin(ang);
+        float co = 1.f, si = 0.f;                    // (pairs that the stage's rotation leaves out)
+        if (!rope.on || tt < rope.dims >> 1) {
+          const double ang = (double)pos * (rope.on ? rope.freq[tt] : exp2(-(2.0 * (double)tt / (double)d_head) * log2((double)theta)));
+          co = (float)cos(ang);
+          si = (float)sin(ang);
+          if (rope.on) { co *= rope.gain; si *= rope.gain; }
+        }
+        cs[(size_t)r * d_head + tt] = co;
+        cs[(size_t)r * d_head + half + tt] = si;
       }
       // the call's plan goes to device memory for the kernels that follow
       if (plan_dev && (int)blockIdx.x == row_blocks) {
@@ -251,8 +259,8 @@ static inline int grid_for(size_t n, int block, int cap = 4096) {
 
 hipError_t sp_launch_enter_norm(int dtype, const void* x, const AttnPlan& plan, AttnPlan* plan_dev,
                                 const ReqMeta* meta, const ReqTables* tables, RowInfo* rows, float* cs, int d_head,
-                                float theta, float* h, const void* gain, void* xn, bool frag, int M, int d, float eps,
-                                hipStream_t st) {
+                                float theta, const StageRope& rope, float* h, const void* gain, void* xn, bool frag, int M, int d,
+                                float eps, hipStream_t st) {
   // 1024 threads per row up to two rows per CU; with more rows 512, so that four rows per CU are in flight (638 rows of
   // 4096, with the tables apart: 13.9 -> 8.4 us) -- as long as a row takes no more than the two passes that stay in
   // registers
@@ -261,11 +269,11 @@ hipError_t sp_launch_enter_norm(int dtype, const void* x, const AttnPlan& plan, 
   static_assert(sizeof(AttnPlan) % 4 == 0 && sizeof(AttnPlan) < 3900, "the plan travels as a kernel argument");
   if (dtype == 0)
     hipLaunchKernelGGL((k_add_norm<float, true>), dim3(M + extra), dim3(nth), 0, st, h, nullptr, 0, 0, (const float*)gain,
-                       (float*)xn, M, d, eps, (const float*)x, plan, plan_dev, meta, tables, rows, cs, d_head, theta, false);
+                       (float*)xn, M, d, eps, (const float*)x, plan, plan_dev, meta, tables, rows, cs, d_head, theta, false, rope);
   else
     hipLaunchKernelGGL((k_add_norm<bf16_t, true>), dim3(norm_blocks(M, frag) + extra), dim3(nth), 0, st, h, nullptr, 0, 0,
                        (const bf16_t*)gain, (bf16_t*)xn, M, d, eps, (const bf16_t*)x, plan, plan_dev, meta, tables, rows,
-                       cs, d_head, theta, frag);
+                       cs, d_head, theta, frag, rope);
   return hipGetLastError();
 }
 
@@ -275,11 +283,11 @@ hipError_t sp_launch_add_norm(int dtype, float* h, const float* part, int S, siz
   if (dtype == 0)
     hipLaunchKernelGGL((k_add_norm<float, false>), dim3(M), dim3(1024), 0, st, h, part, S, part_stride,
                        (const float*)gain, (float*)xn, M, d, eps, nullptr, none, nullptr, nullptr, nullptr, nullptr,
-                       nullptr, 0, 0.f, false);
+                       nullptr, 0, 0.f, false, none);
   else
     hipLaunchKernelGGL((k_add_norm<bf16_t, false>), dim3(norm_blocks(M, frag)), dim3(1024), 0, st, h, part, S, part_stride,
                        (const bf16_t*)gain, (bf16_t*)xn, M, d, eps, nullptr, none, nullptr, nullptr, nullptr, nullptr,
-                       nullptr, 0, 0.f, frag);
+                       nullptr, 0, 0.f, frag, none);
   return hipGetLastError();
 }
 

@@ -268,12 +268,12 @@ __device__ __forceinline__ void rows_compact_slice(const RowsJob& j, const RowLi
                      slice == j.n_slices - 1 ? j.last_slice_bytes : j.slice_bytes, l.first_moved, l.n_keep, s_src);
 }
 
-// grid = (layers * 2 * kv_heads [+ row slices], batch items): one workgroup per (plane, request).
+// grid = (planes [+ row slices], batch items): one workgroup per (plane, request).
 template <bool WITH_ROWS>
 __global__ void __launch_bounds__(256) k_kv_compact(const ReqMeta* meta, const ReqTables* tables, PruneBatch b,
                                                      KvGeom g, RowsJob rj, RowList rl) {
   __shared__ short s_src[SP_T];
-  const int planes = g.n_layers * 2 * g.n_kv_heads;
+  const int planes = g.planes;
   if (WITH_ROWS && (int)blockIdx.x >= planes) {
     rows_compact_slice(rj, rl, blockIdx.x - planes, s_src);
     return;
@@ -322,7 +322,7 @@ hipError_t sp_launch_request_init(ReqMeta* meta, ReqTables* tables, int req, lon
 }
 static_assert(2 * sizeof(void*) + sizeof(InsertArgs) + sizeof(KvGeom) <= 4096, "kernel arguments");
 hipError_t sp_launch_tree_insert(ReqMeta* meta, ReqTables* tables, const InsertArgs& a, KvGeom g, hipStream_t st) {
-  hipLaunchKernelGGL(k_tree_insert, dim3(1 + g.n_layers * 2 * g.n_kv_heads, a.n_req), dim3(SP_T), 0, st, meta, tables,
+  hipLaunchKernelGGL(k_tree_insert, dim3(1 + g.planes, a.n_req), dim3(SP_T), 0, st, meta, tables,
                      a, g);
   return hipGetLastError();
 }
@@ -580,7 +580,7 @@ static RowsJob rows_job(void* rows, size_t row_stride_bytes, int row_bytes) {
 // rows != nullptr (one request only): the hidden rows are compacted by the same launch
 hipError_t sp_launch_kv_compact(const ReqMeta* meta, const ReqTables* tables, const PruneBatch& b, KvGeom g,
                                 void* rows, size_t row_stride_bytes, int row_bytes, const RowList* l, hipStream_t st) {
-  const int planes = g.n_layers * 2 * g.n_kv_heads;
+  const int planes = g.planes;
   if (rows && l && b.n == 1) {
     const RowsJob j = rows_job(rows, row_stride_bytes, row_bytes);
     hipLaunchKernelGGL(k_kv_compact<true>, dim3(planes + j.n_slices, 1), dim3(256), 0, st, meta, tables, b, g, j, *l);
