@@ -10,6 +10,7 @@
 
 #include "../../include/specpipe.h"
 #include "sp_known.h"
+#include "sp_latent_plan.h"
 #include "sp_launch.h"
 
 static_assert(SP_T == SP_MAX_TREE_NODES, "tree capacity");
@@ -1352,8 +1353,10 @@ int sp_latent_attention(sp_stage* s, int32_t layer, int32_t n_req, const int32_t
   AttnPlan plan;
   plan_segments(s, b, nullptr, plan);
   const LatentAttnArgs a = {(const bf16_t*)q, (bf16_t*)out, s->d_tables, s->geom, layer, d, s->lat_scale, s->ws.attn_part};
+  const bool fast = !(s->cfg.flags & SP_FLAG_SIMPLE_KERNELS) && sp_latent_attn_covers(d);
+  if (fast && !latent_split(plan, d.n_heads, d.d_latent, s->n_cu, s->ws.attn_units)) return SP_E_CAPACITY;
   ProfScope p(s, SP_K_ATTENTION, (hipStream_t)stream);
-  const hipError_t e = sp_launch_latent_attn_simple(a, plan, b.n_rows, (hipStream_t)stream);
+  const hipError_t e = fast ? sp_launch_latent_attn(a, plan, b.n_rows, (hipStream_t)stream) : sp_launch_latent_attn_simple(a, plan, b.n_rows, (hipStream_t)stream);
   return e == hipSuccess ? SP_OK : hip_fail(s, e);
 }
 

@@ -251,6 +251,8 @@ struct LatentAttnArgs {
   float scale;
   float* part;                     // partial results of ranges that are cut
 };
+bool sp_latent_attn_covers(const LatentDims& d);     // on the matrix cores, by a plan of latent_split's
+hipError_t sp_launch_latent_attn(const LatentAttnArgs& a, const AttnPlan& plan, int M, hipStream_t st);
 hipError_t sp_launch_latent_attn_simple(const LatentAttnArgs& a, const AttnPlan& plan, int M, hipStream_t st);
 
 // ---- products head by head (sp_head_product.hip) --------------------------------------
