@@ -1,3 +1,5 @@
+#include <type_traits>
+
 #include "sp_launch.h"
 
 typedef __attribute__((ext_vector_type(16))) float f32x16_t;
@@ -17,6 +19,10 @@ __device__ __forceinline__ f32x4_t mfma16(u32x4_t a, u32x4_t b, f32x4_t c) {
 __device__ __forceinline__ f32x16_t mfma32(u32x4_t a, u32x4_t b, f32x16_t c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
 }
+// acc + the two halves of w
+__device__ __forceinline__ float dot2(uint32_t w, float acc) {
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w), __builtin_bit_cast(bf16x2_t, 0x3f803f80u), acc, false);
+}
 __device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u; }
 
 #define LW 8                       // waves per workgroup: four form scores, four the results
@@ -34,6 +40,8 @@ __global__ void __launch_bounds__(64 * LW, 2) k_latent_attn(LatentAttnArgs a, At
   constexpr int SUB = DC / 128, ROW = (DC + DR) * 2, KR = DR / 32, NS = DC / 32 + KR;
   constexpr int SUB_B = LK * 256, TILE = SUB * SUB_B + LK * DR * 2;
   constexpr int CG = DC / 256, RT = R / 32;        // results: CG x 64 columns, RT x 32 rows a wave
+  constexpr int TQ = R / 32;                       // scores: TQ x 16 rows a wave
+  constexpr bool STAGED = R == 64;                 // query rows by way of LDS
   __shared__ __attribute__((aligned(16))) char s_0[TILE], s_1[TILE], s_2[TILE], s_3[TILE];
   __shared__ __attribute__((aligned(16))) char s_p[2][R * LK * 2];
   __shared__ __attribute__((aligned(16))) float s_max[R][2];
@@ -66,7 +74,7 @@ __global__ void __launch_bounds__(64 * LW, 2) k_latent_attn(LatentAttnArgs a, At
   const int rofs = rrow * ROW + DC * 2 + ((lane % U) ^ (U == 8 ? swap128(g8 * 8 + rrow) : swap64(g8 * 8 + rrow))) * 16;
   auto rows_at = [&](const char* p, int n) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), (short)0, n * ROW, 0x00020000); };
   auto rows_of = [&](int tile) {
-    const int at = c0 + tile * LK + g8 * 8, n = uni(max(0, min(8, span - at)));
+    const int at = c0 + tile * LK + g8 * 8, n = uni(tile < tiles ? max(0, min(8, span - at)) : 0);      // (no rows: zeros, without an access)
     const int t0 = uni(n > 0 ? at : 0);
     const size_t slot = PAGED ? ((size_t)pt[t0 >> pg_sh] << pg_sh) + (t0 & pg_mask) : (size_t)t0;
     return rows_at(plane + slot * ROW, n);
@@ -80,15 +88,20 @@ __global__ void __launch_bounds__(64 * LW, 2) k_latent_attn(LatentAttnArgs a, At
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) load(buf, t, i);
   };
-  {
-    const int q0 = qb * R + (R == 64 && wave >= 4 ? 32 : 0) + g8 * 8;
-    const auto buf = rows_at(reinterpret_cast<const char*>(a.q) + ((size_t)row0 * H + q0) * ROW, uni(max(0, min(8, nq - q0))));
-    if (wave < 4) {
-      load_all(buf, s_2);
-      load_all(rows_of(0), s_0);
-    } else {
-      if (R == 64) load_all(buf, s_3);
-      load_all(rows_of(1), s_1);
+  load_all(rows_of(wave < 4 ? 0 : 1), wave < 4 ? s_0 : s_1);
+  if constexpr (STAGED) {
+    const int q0 = qb * R + (wave >> 2) * 32 + g8 * 8;
+    load_all(rows_at(reinterpret_cast<const char*>(a.q) + ((size_t)row0 * H + q0) * ROW, uni(max(0, min(8, nq - q0)))), wave < 4 ? s_2 : s_3);
+  }
+  // scores: TQ x 16 rows x 16 slots of every tile a wave
+  const int rg = wave & 1, kb = (wave >> 1) & 1, row = rg * 16 * TQ + l15;
+  u32x4_t qf[TQ][NS];
+  if (!STAGED && wave < 4) {
+#pragma unroll
+    for (int t = 0; t < TQ; ++t) {
+      const bf16_t* q = a.q + ((size_t)row0 * H + min(qb * R + row + t * 16, nq - 1)) * (DC + DR) + kg * 8;
+#pragma unroll
+      for (int s = 0; s < NS; ++s) qf[t][s] = *reinterpret_cast<const u32x4_t*>(q + s * 32);
     }
   }
   if (c1 > P) {
@@ -115,111 +128,85 @@ __global__ void __launch_bounds__(64 * LW, 2) k_latent_attn(LatentAttnArgs a, At
   };
 
   if (wave < 4) {
-    // ---- scores: 32 rows x 16 slots of every tile
-    const bool on = R == 64 || wave < 2;
-    const int rg = R == 64 ? wave & 1 : 0, kb = R == 64 ? wave >> 1 : wave & 1;
+    // ---- scores
     // places of the lane's units: row l15 of sixteen, columns kg * 8 .. + 7 of 32
     const int ka = l15 * 256 + (kg ^ swap256(l15)) * 16, kr = SUB * SUB_B + l15 * DR * 2 + (kg ^ (DR == 64 ? swap128(l15) : swap64(l15))) * 16;
-    auto unit = [&](const char* t, int s) {
-      return s < SUB * 4 ? *reinterpret_cast<const u32x4_t*>(t + (ka ^ ((s & 3) * 64)) + (s >> 2) * SUB_B)
-                         : *reinterpret_cast<const u32x4_t*>(t + (kr ^ ((s - SUB * 4) * 64)));
+    auto unit = [&](const char* t, int sixteen, int s) {         // of rows sixteen * 16 .. of a tile
+      return s < SUB * 4 ? *reinterpret_cast<const u32x4_t*>(t + sixteen * 4096 + (ka ^ ((s & 3) * 64)) + (s >> 2) * SUB_B)
+                         : *reinterpret_cast<const u32x4_t*>(t + sixteen * 16 * DR * 2 + (kr ^ ((s - SUB * 4) * 64)));
     };
-    u32x4_t qf[2][NS];
+    if constexpr (STAGED) {
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+      for (int t = 0; t < TQ; ++t)
 #pragma unroll
-      for (int s = 0; s < NS; ++s) {
-        const int at = s < SUB * 4 ? t * 4096 : t * 16 * DR * 2;
-        qf[t][s] = unit((rg ? s_3 : s_2) + at, s);
-      }
-    lds_done();
-    bare_barrier();                                // (the query rows' place is free)
-    float shift[2] = {NONE, NONE}, sum[2] = {0.f, 0.f};
-    const int row = rg * 32 + l15;
+        for (int s = 0; s < NS; ++s) qf[t][s] = unit(rg ? s_3 : s_2, t, s);
+      lds_done();
+      bare_barrier();                              // (the query rows' place is free)
+    }
     const int pp = row * 64 + ((kb * 2 + (kg >> 1)) ^ swap64(row)) * 16 + (kg & 1) * 8;      // (row + 16: 1024 behind)
-    auto step = [&](const char* cur, int i) {
-      if (!on) { lds_done(); bare_barrier(); if (uni(s_redo) == i) { bare_barrier(); bare_barrier(); } return; }
-      const int k0 = c0 + i * LK + kb * 16;
-      f32x4_t sv[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-      {
+    float shift[TQ], sum[TQ], add[TQ];
+    f32x4_t sa[TQ], sb[TQ];                        // scores of even and odd tiles
+    bool bad_a = false, bad_b = false;
+#pragma unroll
+    for (int t = 0; t < TQ; ++t) { shift[t] = NONE; sum[t] = add[t] = 0.f; }
+    auto weights = [&](const f32x4_t (&sv)[TQ], int i) {         // of tile i; returns the largest exponent
+      float top = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < TQ; ++t) {
+        float x[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = __builtin_fmaf(sv[t][j], sc, shift[t]);
+        top = fmaxf(fmaxf(fmaxf(top, x[0]), fmaxf(x[1], x[2])), x[3]);
+        uint2 w;
+        w.x = pack_bf16x2(__builtin_amdgcn_exp2f(x[0]), __builtin_amdgcn_exp2f(x[1]));
+        w.y = pack_bf16x2(__builtin_amdgcn_exp2f(x[2]), __builtin_amdgcn_exp2f(x[3]));
+        *reinterpret_cast<uint2*>(s_p[i & 1] + pp + t * 1024) = w;
+        add[t] = dot2(w.x, dot2(w.y, 0.f));
+      }
+      return top;
+    };
+    // tile i on `cur`, and behind its scores the tile before, on `prev`, taken again where that is asked for
+    auto step = [&](char* prev, const f32x4_t (&before)[TQ], bool bad_before, const char* cur, f32x4_t (&sv)[TQ], bool& bad, int i) {
+      const int redo = s_redo;
+      if (i < tiles) {
         constexpr int AHEAD = 6;
         u32x4_t kf[AHEAD];
-        auto key = [&](int s) { return unit(cur + (s < SUB * 4 ? kb * 4096 : kb * 16 * DR * 2), s); };
 #pragma unroll
-        for (int s = 0; s < AHEAD; ++s) kf[s] = key(s);
+        for (int s = 0; s < AHEAD; ++s) kf[s] = unit(cur, kb, s);
+#pragma unroll
+        for (int t = 0; t < TQ; ++t) sv[t] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
 #pragma unroll
-          for (int t = 0; t < 2; ++t) sv[t] = mfma16(kf[s % AHEAD], qf[t][s], sv[t]);
-          if (s + AHEAD < NS) kf[s % AHEAD] = key(s + AHEAD);
+          for (int t = 0; t < TQ; ++t) sv[t] = mfma16(kf[s % AHEAD], qf[t][s], sv[t]);
+          if (s + AHEAD < NS) kf[s % AHEAD] = unit(cur, kb, s + AHEAD);
         }
-        __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, AHEAD + 1, 0);
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
-          __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+          __builtin_amdgcn_sched_group_barrier(0x008, TQ, 0);
           if (s + AHEAD < NS) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
       }
-      bool bad = false;
-      if (k0 + 16 > P || k0 + 16 > c1) {
-        // (what is not finite in a row of the cache shows in all of its scores)
-        float odd = 0.f;
+      if (i > 0 && uni(redo) == i - 1) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) odd += sv[t][j] * 0.f;
-        bad = __builtin_amdgcn_ballot_w64(odd != odd) != 0;
-        const int n0 = k0 - P;
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          uint32_t seen = low_bits(-n0);
-          if (n0 > -32) {
-            const uint32_t* w = &s_anc[row + t * 16][(n0 >> 5) + 1];
-            seen |= __builtin_amdgcn_alignbit(w[1], w[0], n0 & 31);
-          }
-          seen = (seen & low_bits(c1 - k0)) >> (kg * 4);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) sv[t][j] = (seen >> j) & 1u ? sv[t][j] : -INFINITY;
-        }
-      }
-      float add[2], top = -INFINITY;
-      auto weights = [&] {
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          float x[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) x[j] = __builtin_fmaf(sv[t][j], sc, shift[t]);
-          top = fmaxf(fmaxf(fmaxf(top, x[0]), fmaxf(x[1], x[2])), x[3]);
-          uint2 w;
-          w.x = pack_bf16x2(__builtin_amdgcn_exp2f(x[0]), __builtin_amdgcn_exp2f(x[1]));
-          w.y = pack_bf16x2(__builtin_amdgcn_exp2f(x[2]), __builtin_amdgcn_exp2f(x[3]));
-          add[t] = (bf16_lo(w.x) + bf16_hi(w.x)) + (bf16_lo(w.y) + bf16_hi(w.y));
-          *reinterpret_cast<uint2*>(s_p[i & 1] + pp + t * 1024) = w;
-        }
-      };
-      weights();
-      if ((bad || __builtin_amdgcn_ballot_w64(top > FAR)) && lane == 0) s_redo = i;
-      lds_done();
-      bare_barrier();                              // the tile's weights are there, the next tile is, nobody reads the one before
-      if (uni(s_redo) == i) {
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          const float mx = quad_rows_max(fmaxf(fmaxf(sv[t][0], sv[t][1]), fmaxf(sv[t][2], sv[t][3])));
+        for (int t = 0; t < TQ; ++t) {
+          const float mx = quad_rows_max(fmaxf(fmaxf(before[t][0], before[t][1]), fmaxf(before[t][2], before[t][3])));
           if (kg == 0) s_max[row + t * 16][kb] = mx;
         }
         lds_done();
         bare_barrier();                            // maxima are posted
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
+        for (int t = 0; t < TQ; ++t) {
           const float now = shifted(row + t * 16, shift[t]);
           sum[t] *= __builtin_amdgcn_exp2f(now - shift[t]);
           shift[t] = now;
         }
-        weights();
-        if (bad) {
+        weights(before, i - 1);
+        if (bad_before) {
           // values that are not finite count as nothing for those who do not see them (those who do have scores that are none)
           for (int u = lane; u < SUB * 256; u += 64) {
-            u32x4_t* p = reinterpret_cast<u32x4_t*>(const_cast<char*>(cur) + (u >> 8) * SUB_B + kb * 4096) + (u & 255);
+            u32x4_t* p = reinterpret_cast<u32x4_t*>(prev + (u >> 8) * SUB_B + kb * 4096) + (u & 255);
             u32x4_t v = *p;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -230,23 +217,51 @@ __global__ void __launch_bounds__(64 * LW, 2) k_latent_attn(LatentAttnArgs a, At
           }
         }
         lds_done();
-        bare_barrier();
+        bare_barrier();                            // weights are posted
       }
-      sum[0] += add[0];
-      sum[1] += add[1];
-    };
-    for (int i = 0; i < tiles; i += 4) {
-      step(s_0, i);
-      if (i + 1 < tiles) step(s_1, i + 1);
-      if (i + 2 < tiles) step(s_2, i + 2);
-      if (i + 3 < tiles) step(s_3, i + 3);
-    }
-    if (on) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const float l = quad_rows_sum(sum[t]);
-        if (kg == 0) s_max[row + t * 16][kb] = l;
+      for (int t = 0; t < TQ; ++t) sum[t] += add[t];
+      if (i >= tiles) return;
+      const int k0 = c0 + i * LK + kb * 16;
+      bad = false;
+      if (k0 + 16 > P || k0 + 16 > c1) {
+        // (what is not finite in a row of the cache shows in all of its scores)
+        float odd = 0.f;
+#pragma unroll
+        for (int t = 0; t < TQ; ++t)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) odd += sv[t][j] * 0.f;
+        bad = __builtin_amdgcn_ballot_w64(odd != odd) != 0;
+        const int n0 = k0 - P;
+#pragma unroll
+        for (int t = 0; t < TQ; ++t) {
+          uint32_t seen = low_bits(-n0);
+          if (n0 > -32) {
+            const uint32_t* w = &s_anc[row + t * 16][(n0 >> 5) + 1];
+            seen |= __builtin_amdgcn_alignbit(w[1], w[0], n0 & 31);
+          }
+          seen = (seen & low_bits(c1 - k0)) >> (kg * 4);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) sv[t][j] = (seen >> j) & 1u ? sv[t][j] : -INFINITY;
+        }
       }
+      if (i > 0) {                                 // (the first tile is taken again anyway)
+        const float top = weights(sv, i);
+        if ((bad || __builtin_amdgcn_ballot_w64(top > FAR)) && lane == 0) s_redo = i;
+      }
+      lds_done();
+      bare_barrier();                              // the tile's weights are there, the next tile is, nobody reads the one before
+    };
+    for (int i = 0; i <= tiles; i += 4) {
+      step(s_3, sb, bad_b, s_0, sa, bad_a, i);
+      if (i + 1 <= tiles) step(s_0, sa, bad_a, s_1, sb, bad_b, i + 1);
+      if (i + 2 <= tiles) step(s_1, sb, bad_b, s_2, sa, bad_a, i + 2);
+      if (i + 3 <= tiles) step(s_2, sa, bad_a, s_3, sb, bad_b, i + 3);
+    }
+#pragma unroll
+    for (int t = 0; t < TQ; ++t) {
+      const float l = quad_rows_sum(sum[t]);
+      if (kg == 0) s_max[row + t * 16][kb] = l;
     }
     lds_done();
     bare_barrier();
@@ -271,40 +286,18 @@ __global__ void __launch_bounds__(64 * LW, 2) k_latent_attn(LatentAttnArgs a, At
   // places of the lane's transposing reads (unit of 64 columns g: 8 units on, and 128 columns a sub-tile) and of its weights
   const int va = (h * 8 + r) * 256 + ((b * 4 + c) ^ swap256(h * 8 + r)) * 16 + b * 8;
   const int pa = l31 * 64 + (h ^ swap64(l31)) * 16;
-  bare_barrier();                                  // (the query rows' place is free)
-  // the weights of tile i - 1 on `cur`, the loads of tile i + 2 into `next`; then tile i's weights
-  auto step = [&](const char* cur, char* next, int i) {
-    const bool more = i + 2 < tiles;
-    const auto buf = rows_of(more ? i + 2 : 0);
-    if (i > 0) {
-      const char* pw = s_p[(i - 1) & 1];
-#pragma unroll
-      for (int k = 0; k < LK / 16; ++k) {
-        u32x4_t p[RT];
-#pragma unroll
-        for (int t = 0; t < RT; ++t) p[t] = *reinterpret_cast<const u32x4_t*>(pw + (pa ^ (k * 32)) + t * 2048);
-#pragma unroll
-        for (int g = 0; g < CG; ++g)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int at = (va ^ (e * 8) ^ (((c64 + g) & 1) * 128)) + ((c64 + g) >> 1) * SUB_B + k * 4096;
-            const uint2 lo = read_transposed(cur + at), hi = read_transposed(cur + (at ^ 16) + 1024);
-            const u32x4_t v = {lo.x, lo.y, hi.x, hi.y};
-#pragma unroll
-            for (int t = 0; t < RT; ++t) o[g][e][t] = mfma32(v, p[t], o[g][e][t]);
-          }
-      }
-    }
-    if (more) {
-      load_all(buf, next);
-      SP_WAIT_VMEM(LOADS);
-    } else {
-      SP_WAIT_VMEM(0);
-    }
+  if constexpr (STAGED) bare_barrier();            // (the query rows' place is free)
+  auto next_tile = [&] {
+    SP_WAIT_VMEM(LOADS);
     lds_done();
     bare_barrier();                                // the tile's weights are there, the next tile is, nobody reads the one before
-    if (i < tiles && uni(s_redo) == i) {
-      bare_barrier();                              // maxima are posted
+  };
+  // the loads of tile i + 2 into `next`, the weights of tile i - 1 on `cur`
+  auto step = [&](const char* cur, char* next, int i) {
+    const int redo = s_redo;
+    const auto buf = rows_of(i + 2);
+    if (uni(redo) == i - 1) {
+      bare_barrier();                            // maxima are posted
       bool any = false;
       float by[RT];
 #pragma unroll
@@ -323,15 +316,50 @@ __global__ void __launch_bounds__(64 * LW, 2) k_latent_attn(LatentAttnArgs a, At
             for (int t = 0; t < RT; ++t) o[g][e][t] *= by[t];
       }
       lds_done();
-      bare_barrier();
+      bare_barrier();                            // weights are posted
     }
+    // The loads go out among the products: one after the other they hold the wave up, 64 bytes a clock is all that a CU takes.
+    const char* pw = s_p[(i - 1) & 1];
+    constexpr int N = LK / 16 * CG * 2;
+    u32x4_t p[LK / 16][RT];
+#pragma unroll
+    for (int k = 0; k < LK / 16; ++k)
+#pragma unroll
+      for (int t = 0; t < RT; ++t) p[k][t] = *reinterpret_cast<const u32x4_t*>(pw + (pa ^ (k * 32)) + t * 2048);
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int k = n / (CG * 2), g = n / 2 % CG, e = n & 1;
+      const int at = (va ^ (e * 8) ^ (((c64 + g) & 1) * 128)) + ((c64 + g) >> 1) * SUB_B + k * 4096;
+      const uint2 lo = read_transposed(cur + at), hi = read_transposed(cur + (at ^ 16) + 1024);
+      const u32x4_t v = {lo.x, lo.y, hi.x, hi.y};
+#pragma unroll
+      for (int t = 0; t < RT; ++t) o[g][e][t] = mfma32(v, p[k][t], o[g][e][t]);
+      load(buf, next, n);
+    }
+    static_assert(LOADS == N + 1, "a load for every fragment, and one");
+    load(buf, next, N);
+    __builtin_amdgcn_sched_group_barrier(0x100, LK / 16 * RT + 4, 0);
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      __builtin_amdgcn_sched_group_barrier(0x008, RT, 0);
+      if (n + 2 < N) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);
+    }
+    next_tile();
   };
-  for (int i = 0; i <= tiles; i += 4) {
+  load_all(rows_of(2), s_2);
+  next_tile();
+  for (int i = 1;;) {
+    step(s_0, s_3, i);
+    if (++i > tiles) break;
+    step(s_1, s_0, i);
+    if (++i > tiles) break;
+    step(s_2, s_1, i);
+    if (++i > tiles) break;
     step(s_3, s_2, i);
-    if (i + 1 <= tiles) step(s_0, s_3, i + 1);
-    if (i + 2 <= tiles) step(s_1, s_0, i + 2);
-    if (i + 3 <= tiles) step(s_2, s_1, i + 3);
+    if (++i > tiles) break;
   }
+  SP_WAIT_VMEM(0);                                 // (zeros, on their way to a place that the workgroup gives away)
 
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
@@ -364,56 +392,113 @@ __global__ void __launch_bounds__(64 * LW, 2) k_latent_attn(LatentAttnArgs a, At
   }
 }
 
-// A wave joins the chunks of a query row, DC / 64 columns a lane: first every lane one chunk's weight, then the rows in their order.
-template <int DC>
-__global__ void __launch_bounds__(256) k_latent_merge(LatentAttnArgs a, AttnPlan plan, int n) {
-  constexpr int V = DC / 64;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, H = a.d.n_heads;
-  const int at = blockIdx.x * 4 + wave;            // row * H + head of the call
-  if (at >= n) return;
+// A query row of the call, row * H + head: the request it belongs to, and its partial rows.
+struct LatentRow { int chunks; size_t u0, stride; };
+__device__ __forceinline__ LatentRow latent_row(const AttnPlan& plan, int at, int H, int lane) {
   const int row = at / H;
   int seg = 0;
   if (plan.n_seg > 1) {
     const int first = plan.seg_row0[lane];
     seg = __ffsll((unsigned long long)__builtin_amdgcn_ballot_w64(lane < plan.n_seg && row >= first && row < first + plan.seg_rows[lane])) - 1;
   }
-  const int chunks = plan.seg_chunks[seg];
-  if (chunks == 1) return;
-  const size_t stride = (size_t)plan.seg_rows[seg] * H, u0 = (size_t)plan.seg_unit0[seg] + at - (size_t)plan.seg_row0[seg] * H;
+  return {plan.seg_chunks[seg], (size_t)plan.seg_unit0[seg] + at - (size_t)plan.seg_row0[seg] * H, (size_t)plan.seg_rows[seg] * H};
+}
+
+// Few chunks: a wave joins those of a query row, DC / 64 columns a lane, four chunks on their way at a time.
+#define LATENT_FEW 16
+template <int DC>
+__global__ void __launch_bounds__(256) k_latent_merge_few(LatentAttnArgs a, AttnPlan plan, int n) {
+  constexpr int V = DC / 256;                      // four columns at lane * 4 + 256 v
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, at = blockIdx.x * 4 + wave;
+  if (at >= n) return;
+  const LatentRow r = latent_row(plan, at, a.d.n_heads, lane);
+  if (r.chunks == 1) return;
   const float* ml = a.part + (size_t)plan.units_total * DC;
-  float acc[V], l = 0.f, mx = -INFINITY;
+  float m = -INFINITY, s = 0.f;
+  if (lane < r.chunks) {
+    const float2 x = *reinterpret_cast<const float2*>(ml + (r.u0 + lane * r.stride) * 2);
+    m = x.x; s = x.y;
+  }
+  const float* po = a.part + r.u0 * DC + lane * 4;
+  f32x4_t acc[V];
 #pragma unroll
-  for (int i = 0; i < V; ++i) acc[i] = 0.f;
-  for (int b = 0; b < chunks; b += 64) {
-    float m = -INFINITY, s = 0.f;
-    if (b + lane < chunks) {
-      const float2 x = *reinterpret_cast<const float2*>(ml + (u0 + (b + lane) * stride) * 2);
-      m = x.x; s = x.y;
-    }
-    const float top = fmaxf(mx, wave_max(m)), f = mx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mx - top);
-    l *= f;
+  for (int v = 0; v < V; ++v) acc[v] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+  float w = 0.f;
+  for (int j = 0; j < r.chunks; j += 4) {
+    f32x4_t x[4][V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) acc[i] *= f;
-    mx = top;
-    const float w = b + lane < chunks ? __builtin_amdgcn_exp2f(m - top) : 0.f;
-    l += wave_sum(w * s);
-    const int nb = min(64, chunks - b);
-    for (int j = 0; j < nb; ++j) {
-      const float wj = __shfl(w, j, 64);
-      const float* po = a.part + (u0 + (size_t)(b + j) * stride) * DC + lane * V;
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int i = 0; i < V; i += 4) {
-        const f32x4_t x = *reinterpret_cast<const f32x4_t*>(po + i);
+      for (int v = 0; v < V; ++v) x[i][v] = *reinterpret_cast<const f32x4_t*>(po + (size_t)min(j + i, r.chunks - 1) * r.stride * DC + v * 256);
+    if (j == 0) w = __builtin_amdgcn_exp2f(m - wave_max(m));     // (lanes without a chunk: zero)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[i + e] += wj * x[e];
-      }
+    for (int i = 0; i < 4; ++i) {
+      const float wi = __shfl(w, j + i, 64);       // (none: zero)
+#pragma unroll
+      for (int v = 0; v < V; ++v) acc[v] += wi * x[i][v];
     }
   }
-  const float inv = 1.f / l;
-  bf16_t* out = a.out + (size_t)at * DC + lane * V;
+  const float inv = 1.f / wave_sum(w * s);
 #pragma unroll
-  for (int i = 0; i < V; i += 4)
-    *reinterpret_cast<uint2*>(out + i) = uint2{pack_bf16x2(acc[i] * inv, acc[i + 1] * inv), pack_bf16x2(acc[i + 2] * inv, acc[i + 3] * inv)};
+  for (int v = 0; v < V; ++v)
+    *reinterpret_cast<uint2*>(a.out + (size_t)at * DC + lane * 4 + v * 256) =
+        uint2{pack_bf16x2(acc[v][0] * inv, acc[v][1] * inv), pack_bf16x2(acc[v][2] * inv, acc[v][3] * inv)};
+}
+
+// Many: a workgroup joins those of a query row, a thread four columns, groups of threads every second chunk (DC 256: fourth), eight on
+// their way at a time.
+template <int DC>
+__global__ void __launch_bounds__(256) k_latent_merge(LatentAttnArgs a, AttnPlan plan) {
+  constexpr int T = DC / 4, G = 256 / T;           // threads of a row, groups of chunks
+  __shared__ float s_w[256], s_red[8];
+  __shared__ __attribute__((aligned(16))) float s_acc[(G - 1) * DC];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, at = blockIdx.x;
+  const LatentRow r = latent_row(plan, at, a.d.n_heads, lane);
+  if (r.chunks == 1) return;
+  const int chunks = r.chunks;
+  const size_t stride = r.stride, u0 = r.u0;
+  const float* ml = a.part + (size_t)plan.units_total * DC;
+  const int col = (threadIdx.x % T) * 4, group = threadIdx.x / T;
+  f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+  float l = 0.f, mx = -INFINITY;
+  for (int b = 0; b < chunks; b += 256) {
+    const int nb = min(256, chunks - b);
+    float m = -INFINITY, s = 0.f;
+    if ((int)threadIdx.x < nb) {
+      const float2 x = *reinterpret_cast<const float2*>(ml + (u0 + (b + threadIdx.x) * stride) * 2);
+      m = x.x; s = x.y;
+    }
+    const float wm = wave_max(m);
+    if (lane == 0) s_red[wave] = wm;
+    __syncthreads();
+    const float top = fmaxf(fmaxf(fmaxf(s_red[0], s_red[1]), fmaxf(s_red[2], s_red[3])), mx);
+    const float f = mx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mx - top), w = (int)threadIdx.x < nb ? __builtin_amdgcn_exp2f(m - top) : 0.f;
+    s_w[threadIdx.x] = w;
+    const float ws = wave_sum(w * s);
+    if (lane == 0) s_red[4 + wave] = ws;
+    __syncthreads();
+    l = l * f + ((s_red[4] + s_red[5]) + (s_red[6] + s_red[7]));
+    acc *= f;
+    mx = top;
+    const float* po = a.part + (u0 + (size_t)b * stride) * DC + col;
+    int j = group;
+    for (; j + 7 * G < nb; j += 8 * G) {
+      f32x4_t x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const f32x4_t*>(po + (size_t)(j + i * G) * stride * DC);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) acc += s_w[j + i * G] * x[i];
+    }
+    for (; j < nb; j += G) acc += s_w[j] * *reinterpret_cast<const f32x4_t*>(po + (size_t)j * stride * DC);
+    __syncthreads();
+  }
+  if (group > 0) *reinterpret_cast<f32x4_t*>(s_acc + (group - 1) * DC + col) = acc;
+  __syncthreads();
+  if (group > 0) return;
+#pragma unroll
+  for (int g = 1; g < G; ++g) acc += *reinterpret_cast<const f32x4_t*>(s_acc + (g - 1) * DC + col);
+  const float inv = 1.f / l;
+  *reinterpret_cast<uint2*>(a.out + (size_t)at * DC + col) = uint2{pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};
 }
 
 bool sp_latent_attn_covers(const LatentDims& d) { return (d.d_latent == 512 || d.d_latent == 256) && (d.d_rope == 64 || d.d_rope == 32); }
@@ -426,7 +511,10 @@ static hipError_t go(const LatentAttnArgs& a, const AttnPlan& plan, int M, hipSt
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !plan.any_split) return e;
   const int n = M * a.d.n_heads;
-  hipLaunchKernelGGL((k_latent_merge<DC>), dim3((n + 3) / 4), dim3(256), 0, st, a, plan, n);
+  int most = 0;
+  for (int i = 0; i < plan.n_seg; ++i) most = plan.seg_chunks[i] > most ? plan.seg_chunks[i] : most;
+  if (most <= LATENT_FEW) hipLaunchKernelGGL((k_latent_merge_few<DC>), dim3((n + 3) / 4), dim3(256), 0, st, a, plan, n);
+  else hipLaunchKernelGGL((k_latent_merge<DC>), dim3(n), dim3(256), 0, st, a, plan);
   return hipGetLastError();
 }
 template <int DC, int DR>
