@@ -130,7 +130,7 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
         "sp_stage_append": [vp, C.c_int32, C.c_int32, vp, vp, vp, vp, vp, vp],
         "sp_stage_attention": [vp, C.c_int32, C.c_int32, vp, vp, vp, vp, vp, vp],
         "sp_rope_frequencies": [C.c_int32, C.c_double, C.c_int32, C.c_double, C.c_double, C.c_double, C.c_double, C.POINTER(C.c_double)],
-        "sp_rotate": [C.POINTER(sp_rope), C.c_int32, C.c_int32, vp, C.c_int64, C.c_int64, C.c_int32, C.c_int32, C.c_int32, vp, vp, C.c_int64,
+        "sp_rotate": [vp, C.c_int32, C.c_int32, vp, C.c_int64, C.c_int64, C.c_int32, C.c_int32, C.c_int32, vp, vp, C.c_int64,
                       C.c_int64, vp],
         "sp_stage_set_rope": [vp, C.POINTER(sp_rope)],
         "sp_latent_query_sizes": [C.POINTER(sp_config), C.POINTER(sp_latent), C.POINTER(sp_sizes)],
@@ -248,6 +248,7 @@ class Rope:
     def __init__(self, layout: str, dims: int, theta: float = 0.0, scaling: Optional[tuple] = None, gain: float = 1.0,
                  freq: Optional[Sequence[float]] = None):
         self.c = sp_rope(ROPE_LAYOUTS[layout], dims, gain, 0)
+        self.at = C.addressof(self.c)
         if freq is not None:
             if len(freq) * 2 != dims or len(freq) > SP_ROPE_MAX_PAIRS:
                 raise SpError(-1, "a rotation of %d columns at %d frequencies" % (dims, len(freq)))
@@ -806,50 +807,71 @@ def fp4_product(x, w: Fp4Matrix, gated: bool = False, out=None):
 
 
 # ---- rotary positions and products head by head ---------------------------------------------
-def _heads(t, rows: int, heads: int, cols: int, dtype, device) -> tuple:
-    """(address, row stride, head stride) of [rows, heads, cols] whose heads lie one element after the other."""
-    assert t.is_cuda and t.device == device and t.dtype is dtype and t.dim() == 3
-    assert t.shape[0] == rows and t.shape[1] == heads and t.shape[2] == cols and t.stride(2) == 1
+# (These calls take as long as their way through Python: devices as numbers, strides asked for once, nothing checked of a result that
+# is made here.)
+_torch = None
+
+
+def _with_torch():
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    return _torch
+
+
+def _strides(t, rows: int, heads: int) -> tuple:
+    """(row stride, head stride) of [rows, heads, columns] whose heads lie one element after the other."""
+    s = t.stride()
+    assert s[2] == 1 or t.shape[2] == 1
     # (the stride of an axis of one entry says nothing: torch's may be anything)
-    return t.data_ptr(), t.stride(0) if rows > 1 else 0, t.stride(1) if heads > 1 else 0
+    return s[0] if rows > 1 else 0, s[1] if heads > 1 else 0
 
 
 def rotate(x, positions, rope: Rope, inverse: bool = False, out=None):
     """sp_rotate: x [rows, heads, d_head] (bf16 or float32, rows and heads of any stride) turned at positions [rows] (int32, on x's
     device); inverse: back, by which gradients come back.  out may be x."""
-    import torch
-    device = x.device
-    assert x.is_cuda and positions.device == device
-    if device.index != torch._C._cuda_getDevice():
+    torch = _torch or _with_torch()
+    device = x.get_device()
+    assert device >= 0 and positions.get_device() == device
+    if device != torch._C._cuda_getDevice():
         with torch.cuda.device(device):
             return rotate(x, positions, rope, inverse, out)
     rows, heads, d = x.shape
-    assert x.dtype in (torch.bfloat16, torch.float32)
+    dtype = x.dtype
+    assert dtype is torch.bfloat16 or dtype is torch.float32
     assert positions.dtype is torch.int32 and positions.shape == (rows,) and positions.is_contiguous()
+    xr, xh = _strides(x, rows, heads)
     if out is None:
-        out = torch.empty(rows, heads, d, dtype=x.dtype, device=device)
-    _check(load_library().sp_rotate(C.byref(rope.c), SP_BF16 if x.dtype is torch.bfloat16 else SP_F32, 1 if inverse else 0,
-                                    *_heads(x, rows, heads, d, x.dtype, device), rows, heads, d, positions.data_ptr(),
-                                    *_heads(out, rows, heads, d, x.dtype, device), torch._C._cuda_getCurrentRawStream(device.index)), "sp_rotate")
+        out, our, ouh = torch.empty((rows, heads, d), dtype=dtype, device=x.device), heads * d, d
+    else:
+        assert out.get_device() == device and out.dtype is dtype and out.shape == (rows, heads, d)
+        our, ouh = _strides(out, rows, heads)
+    _check(load_library().sp_rotate(rope.at, 1 if dtype is torch.bfloat16 else 0, 1 if inverse else 0, x.data_ptr(), xr, xh, rows, heads, d,
+                                    positions.data_ptr(), out.data_ptr(), our, ouh, torch._C._cuda_getCurrentRawStream(device)), "sp_rotate")
     return out
 
 
 def head_product(x, w, out=None):
     """sp_head_product: x [m, heads, k] bf16 (rows and heads of any stride) times w [heads, n, k], head by head: [m, heads, n]."""
-    import torch
-    device = x.device
-    assert x.is_cuda and w.device == device
-    if device.index != torch._C._cuda_getDevice():
+    torch = _torch or _with_torch()
+    device = x.get_device()
+    assert device >= 0 and w.get_device() == device
+    if device != torch._C._cuda_getDevice():
         with torch.cuda.device(device):
             return head_product(x, w, out)
     m, heads, k = x.shape
     n = w.shape[1]
-    assert w.dtype is torch.bfloat16 and w.shape == (heads, n, k) and w.is_contiguous()
+    bf16 = torch.bfloat16
+    assert x.dtype is bf16 and w.dtype is bf16 and w.shape == (heads, n, k) and w.is_contiguous()
+    xr, xh = _strides(x, m, heads)
     if out is None:
-        out = torch.empty(m, heads, n, dtype=torch.bfloat16, device=device)
-    xp, xr, xh = _heads(x, m, heads, k, torch.bfloat16, device)
-    _check(load_library().sp_head_product(xp, xr, xh, m, heads, w.data_ptr(), n, k, *_heads(out, m, heads, n, torch.bfloat16, device),
-                                          torch._C._cuda_getCurrentRawStream(device.index)), "sp_head_product")
+        out, our, ouh = torch.empty((m, heads, n), dtype=bf16, device=x.device), heads * n, n
+    else:
+        assert out.get_device() == device and out.dtype is bf16 and out.shape == (m, heads, n)
+        our, ouh = _strides(out, m, heads)
+    _check(load_library().sp_head_product(x.data_ptr(), xr, xh, m, heads, w.data_ptr(), n, k, out.data_ptr(), our, ouh,
+                                          torch._C._cuda_getCurrentRawStream(device)), "sp_head_product")
     return out
 
 
@@ -890,11 +912,9 @@ class LatentStage(Stage):
             bufs = sp_buffers(self.kv.data_ptr(), sz.kv_bytes, self.tables.data_ptr(), sz.tables_bytes, self.workspace.data_ptr(), sz.workspace_bytes)
             _check(self.lib.sp_latent_stage_create(C.byref(self.cfg), C.byref(lat), C.byref(bufs), self._stream(), C.byref(h)), "sp_latent_stage_create")
         self.handle = h
+        self.index = self.kv.get_device()
         if rope is not None:
             self.set_rope(rope)
-
-    def _elsewhere(self) -> bool:
-        return self.device.index is not None and self.device.index != self.torch._C._cuda_getDevice()
 
     def kv_view(self):
         """The slab as a tensor [layer, slot, d_latent + d_rope] (no copy)."""
@@ -918,38 +938,48 @@ class LatentStage(Stage):
         _check(self.lib.sp_latent_load(self.handle, req, layer, first_slot, n, rows.data_ptr(), self._stream()), "sp_latent_load")
         return rows
 
+    def _call(self, req_ids, first_node, n_nodes) -> tuple:
+        r, f, n = _ids(req_ids), _ids(first_node), _ids(n_nodes)
+        assert len(r) == len(f) == len(n)
+        return r, f, n, sum(n)
+
     def append(self, layer: int, req_ids: Sequence[int], first_node: Sequence[int], n_nodes: Sequence[int], q, kv, q_out=None):
         """sp_latent_append: q [sum n_nodes, n_heads, d_rope] (a view: rows and heads of any stride) is rotated into q_out (default: a new
         tensor); kv [sum n_nodes, d_latent + d_rope] (rows of any stride) goes to the nodes' cache slots."""
-        if self._elsewhere():
-            with self.torch.cuda.device(self.device):
+        torch, device, dtype = self.torch, self.index, self.tdtype
+        if device != torch._C._cuda_getDevice():
+            with torch.cuda.device(self.device):
                 return self.append(layer, req_ids, first_node, n_nodes, q, kv, q_out)
-        r, n, rows = self._counted(req_ids, n_nodes)
-        f = _ids(first_node)
-        assert len(f) == len(r)
+        r, f, n, rows = self._call(req_ids, first_node, n_nodes)
+        heads, cols = self.n_heads, self.d_rope
+        assert q.get_device() == device and q.dtype is dtype and q.shape == (rows, heads, cols)
+        assert kv.get_device() == device and kv.dtype is dtype and kv.shape == (rows, self.d_latent + cols) and kv.stride(1) == 1
+        qr, qh = _strides(q, rows, heads)
         if q_out is None:
-            q_out = self.torch.empty(max(rows, 0), self.n_heads, self.d_rope, dtype=self.tdtype, device=self.device)
-        at = kv.device
-        assert kv.is_cuda and kv.dtype is self.tdtype and kv.shape == (rows, self.d_latent + self.d_rope) and kv.stride(1) == 1
-        _check(self.lib.sp_latent_append(self.handle, layer, len(r), _at(r), _at(f), _at(n), *_heads(q, rows, self.n_heads, self.d_rope, self.tdtype, at),
-                                         kv.data_ptr(), kv.stride(0) if rows > 1 else 0,
-                                         *_heads(q_out, rows, self.n_heads, self.d_rope, self.tdtype, at), self._stream()), "sp_latent_append")
+            q_out, our, ouh = torch.empty((rows, heads, cols), dtype=dtype, device=self.device), heads * cols, cols
+        else:
+            assert q_out.get_device() == device and q_out.dtype is dtype and q_out.shape == (rows, heads, cols)
+            our, ouh = _strides(q_out, rows, heads)
+        _check(self.lib.sp_latent_append(self.handle, layer, len(r), _at(r), _at(f), _at(n), q.data_ptr(), qr, qh, kv.data_ptr(),
+                                         kv.stride(0) if rows > 1 else 0, q_out.data_ptr(), our, ouh, torch._C._cuda_getCurrentRawStream(device)),
+               "sp_latent_append")
         return q_out
 
     def attention(self, layer: int, req_ids: Sequence[int], first_node: Sequence[int], n_nodes: Sequence[int], q, out=None):
         """sp_latent_attention: q [sum n_nodes, n_heads, d_latent + d_rope] -> [sum n_nodes, n_heads, d_latent]."""
-        if self._elsewhere():
-            with self.torch.cuda.device(self.device):
+        torch, device, dtype = self.torch, self.index, self.tdtype
+        if device != torch._C._cuda_getDevice():
+            with torch.cuda.device(self.device):
                 return self.attention(layer, req_ids, first_node, n_nodes, q, out)
-        r, n, rows = self._counted(req_ids, n_nodes)
-        f = _ids(first_node)
-        assert len(f) == len(r)
+        r, f, n, rows = self._call(req_ids, first_node, n_nodes)
+        heads, cols = self.n_heads, self.d_latent
+        assert q.get_device() == device and q.dtype is dtype and q.shape == (rows, heads, cols + self.d_rope) and q.is_contiguous()
         if out is None:
-            out = self.torch.empty(max(rows, 0), self.n_heads, self.d_latent, dtype=self.tdtype, device=self.device)
-        for t, cols in ((q, self.d_latent + self.d_rope), (out, self.d_latent)):
-            assert t.is_cuda and t.dtype is self.tdtype and t.shape == (rows, self.n_heads, cols) and t.is_contiguous()
-        _check(self.lib.sp_latent_attention(self.handle, layer, len(r), _at(r), _at(f), _at(n), q.data_ptr(), out.data_ptr(), self._stream()),
-               "sp_latent_attention")
+            out = torch.empty((rows, heads, cols), dtype=dtype, device=self.device)
+        else:
+            assert out.get_device() == device and out.dtype is dtype and out.shape == (rows, heads, cols) and out.is_contiguous()
+        _check(self.lib.sp_latent_attention(self.handle, layer, len(r), _at(r), _at(f), _at(n), q.data_ptr(), out.data_ptr(),
+                                            torch._C._cuda_getCurrentRawStream(device)), "sp_latent_attention")
         return out
 
 

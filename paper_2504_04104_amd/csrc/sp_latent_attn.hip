@@ -1,5 +1,6 @@
 #include <type_traits>
 
+#include "sp_latent_plan.h"
 #include "sp_launch.h"
 
 typedef __attribute__((ext_vector_type(16))) float f32x16_t;
@@ -56,7 +57,9 @@ __global__ void __launch_bounds__(64 * LW, 2) k_latent_attn(LatentAttnArgs a, At
   if (plan.n_seg > 1) seg = uni(__popcll(__builtin_amdgcn_ballot_w64(lane < plan.n_seg && item >= plan.seg_item0[lane])) - 1);
   const int chunks = plan.seg_chunks[seg], seg_rows = plan.seg_rows[seg], row0 = plan.seg_row0[seg], req = plan.seg_req[seg];
   const int P = plan.seg_P[seg], span = P + plan.seg_T[seg], clen = plan.seg_clen[seg];
-  const int local = item - plan.seg_item0[seg], qb = uni(local / chunks), ch = local - qb * chunks;
+  const LatentItem work = latent_item(item - plan.seg_item0[seg], plan.seg_qblocks[seg], chunks);
+  const int qb = uni(work.block), ch = uni(work.chunk);
+  if (ch >= chunks) return;
   const int H = a.d.n_heads, nq = seg_rows * H;    // query rows of the request, node * H + head
   const int c0 = ch * clen, c1 = min(c0 + clen, span), tiles = (c1 - c0 + LK - 1) / LK;
 

@@ -4,6 +4,21 @@
 
 #define LATENT_TILE 64             // slots that a workgroup takes at a time
 
+// Workgroups of a request, (block of query rows, chunk) by number: chunk after chunk for every block, or, where there are eight chunks and
+// more, eight chunks side by side for every block, so that a chunk's blocks run on the XCD whose L2 has it (consecutive workgroups go
+// round over the eight; 80 rows behind 32749 slots in 64 chunks 24.7 us, in 74, which scattered them, 30.3).  The last eight chunks
+// may be part empty: chunk >= chunks then, nothing to do.
+struct LatentItem { int block, chunk; };
+#ifdef __HIPCC__
+__host__ __device__
+#endif
+inline LatentItem latent_item(int local, int blocks, int chunks) {
+  if (chunks < 8 || blocks == 1) return {local / chunks, local % chunks};
+  const int eights = local >> 3;
+  return {eights % blocks, eights / blocks * 8 + (local & 7)};
+}
+inline int latent_items(int blocks, int chunks) { return (chunks < 8 || blocks == 1 ? chunks : (chunks + 7) / 8 * 8) * blocks; }
+
 // Every request's range in chunks of at most `len` tiles, blocks of `rows` query rows; returns the partial rows that this takes.
 inline size_t latent_cut(AttnPlan& plan, int H, int rows, int len) {
   size_t units = 0;
@@ -15,7 +30,7 @@ inline size_t latent_cut(AttnPlan& plan, int H, int rows, int len) {
     const int qblocks = (int)(((long long)plan.seg_rows[i] * H + rows - 1) / rows);
     plan.seg_item0[i] = items; plan.seg_chunks[i] = chunks; plan.seg_clen[i] = each * LATENT_TILE; plan.seg_qblocks[i] = qblocks;
     plan.seg_unit0[i] = (int)units;
-    items += chunks * qblocks;
+    items += latent_items(qblocks, chunks);
     if (chunks > 1) { units += (size_t)chunks * plan.seg_rows[i] * H; split = 1; }
   }
   plan.total_items = items;
@@ -25,6 +40,9 @@ inline size_t latent_cut(AttnPlan& plan, int H, int rows, int len) {
   return units;
 }
 
+// Blocks of 32 or 64 query rows and chunks of the ranges, by the time that they would take: a tile of 64 slots is 1.3 us of a workgroup of
+// 32 rows and 1.75 of one of 64 (d_latent 512; what LDS gives a clock bounds both), a workgroup has 4.5 us beside its tiles, a CU
+// room for one; chunks cost the merge, a launch and the partial rows on their way out and back.  False: the partial rows do not fit.
 inline bool latent_split(AttnPlan& plan, int H, int d_latent, int n_cu, size_t room) {
   int longest = 1;
   for (int i = 0; i < plan.n_seg; ++i) {
@@ -32,16 +50,16 @@ inline bool latent_split(AttnPlan& plan, int H, int d_latent, int n_cu, size_t r
     longest = tiles > longest ? tiles : longest;
   }
   double best = 1e30;
-  int best_rows = 0, best_len = 0;
+  int best_rows = 64, best_len = longest;
   for (int rows = 32; rows <= 64; rows += 32) {
     double work = 0.;
-    for (int i = 0; i < plan.n_seg; ++i) {
-      const long long qb = ((long long)plan.seg_rows[i] * H + rows - 1) / rows;
-      work += (double)qb * ((plan.seg_P[i] + plan.seg_T[i] + LATENT_TILE - 1) / LATENT_TILE);
-    }
-    const double tile = rows == 32 ? 1.1 : 1.4;
-    for (int cuts = 1; cuts <= longest; cuts = cuts < 4 ? cuts + 1 : cuts + cuts / 3) {
-      const int len = (longest + cuts - 1) / cuts;
+    for (int i = 0; i < plan.n_seg; ++i)
+      work += (double)(((long long)plan.seg_rows[i] * H + rows - 1) / rows) * ((plan.seg_P[i] + plan.seg_T[i] + LATENT_TILE - 1) / LATENT_TILE);
+    const double tile = (rows == 32 ? 1.3 : 1.75) * (0.15 + 0.85 / 512. * d_latent);
+    for (int cuts = 1, len = longest, before = 0; cuts <= longest; cuts = cuts < 8 ? cuts + 1 : cuts + cuts / 4) {
+      len = (longest + cuts - 1) / cuts;
+      if (len == before) continue;
+      before = len;
       long long items = 0;
       double units = 0.;
       for (int i = 0; i < plan.n_seg; ++i) {
@@ -49,15 +67,14 @@ inline bool latent_split(AttnPlan& plan, int H, int d_latent, int n_cu, size_t r
         items += ((long long)plan.seg_rows[i] * H + rows - 1) / rows * chunks;
         if (chunks > 1) units += (double)chunks * plan.seg_rows[i] * H;
       }
-      if (units > (double)room && cuts > 1) break;
+      if (units > (double)room) break;
       const double rounds = (double)items / n_cu;
       double t = rounds <= 1. ? len : work / n_cu + 0.5 * len;
       if (t < len) t = len;
-      t = t * tile + 2. * (rounds <= 1. ? 1. : rounds);
-      if (units > 0.) t += 5. + units * d_latent * 8. / 4e6;
+      t = t * tile + 4.5 * (rounds <= 1. ? 1. : rounds);
+      if (units > 0.) t += 4.5 + units * d_latent * 8. / 4.5e6;
       if (t < best) { best = t; best_rows = rows; best_len = len; }
     }
   }
-  const size_t units = latent_cut(plan, H, best_rows, best_len);
-  return units <= room;
+  return latent_cut(plan, H, best_rows, best_len) <= room;
 }
