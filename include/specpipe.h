@@ -306,13 +306,12 @@ typedef enum sp_rope_scaling { SP_ROPE_PLAIN = 0, SP_ROPE_LINEAR = 1, SP_ROPE_BA
 int sp_rope_frequencies(int32_t dims, double theta, int32_t scaling, double factor, double original, double first, double second,
                         double* freq_out /*host, dims / 2*/);
 
-/* Rows of heads rotated at positions of their own: x and out [n_rows][n_heads] of d_head columns (a multiple of 8, up to 256),
- * strides between rows and between heads in elements, multiples of 8 and at least 0 (out: no two heads on the same elements);
+/* Rows of heads rotated at positions of their own: x and out [n_rows][n_heads] (up to 65536) of d_head columns (a multiple of 8, up to
+ * 256), strides between rows and between heads in elements, multiples of 8 and at least 0 (out: no two heads on the same elements);
  * positions [n_rows] (device).  out may be x, with x's strides (in place), and may not overlap it otherwise, from its first element
- * to its last.  inverse = 1 turns
- * back by the same angles with the same gain: the transpose, by which gradients come back.  Pointers are 16-byte aligned device
+ * to its last.  inverse = 1 turns back by the same angles with the same gain: the transpose, by which gradients come back.  Pointers are 16-byte aligned device
  * memory.  Keys for sp_kv_store are rotated with it, and what a stage does not compute.  n_rows == 0 does nothing.  Errors: SP_E_INVALID,
- * SP_E_UNSUPPORTED (d_head, strides). */
+ * SP_E_UNSUPPORTED (n_heads, d_head, strides). */
 int sp_rotate(const sp_rope* rope, int32_t dtype, int32_t inverse, const void* x, int64_t x_row, int64_t x_head, int32_t n_rows,
               int32_t n_heads, int32_t d_head, const int32_t* positions /*device*/, void* out, int64_t out_row, int64_t out_head,
               sp_stream stream);

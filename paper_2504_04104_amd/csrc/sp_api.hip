@@ -1241,7 +1241,7 @@ static int check_rope(const sp_rope* r, int cols) {
 int sp_rotate(const sp_rope* rope, int32_t dtype, int32_t inverse, const void* x, int64_t x_row, int64_t x_head, int32_t n_rows, int32_t n_heads,
               int32_t d_head, const int32_t* positions, void* out, int64_t out_row, int64_t out_head, sp_stream stream) {
   if (n_rows < 0 || n_heads < 1 || d_head < 8 || (dtype != SP_F32 && dtype != SP_BF16) || (inverse != 0 && inverse != 1)) return SP_E_INVALID;
-  if (d_head % 8 || d_head > 2 * SP_ROPE_MAX_PAIRS) return SP_E_UNSUPPORTED;
+  if (d_head % 8 || d_head > 2 * SP_ROPE_MAX_PAIRS || n_heads > 65536) return SP_E_UNSUPPORTED;
   const int rc = check_rope(rope, d_head);
   if (rc != SP_OK) return rc;
   if (n_rows == 0) return SP_OK;

@@ -1,16 +1,20 @@
 // Products head by head: out[m][h] = x[m][h] W[h]^T, bf16 with float32 sums.
+//
+// Every weight is used m times and every value of x n times: up to some hundred rows the call is bound by the weights' and results' way
+// through memory, and by its launch.  One row x 16 heads, 128 -> 512: 2.6 us; 64 rows x 64 heads, 512 -> 128: 5.8 (14 MB); 637 x 64, 128 ->
+// 512: 17 to 19 (60 MB, 3.3 TB/s, two thirds of it results).
 #include "sp_launch.h"
 
 typedef __attribute__((ext_vector_type(16))) float f32x16_t;
 
-// ---- up to 32 rows: a wave has 16 rows x 16 columns of a head ------------------------------
+// ---- up to 16 rows: a wave has 16 rows x 16 columns of a head ------------------------------
 // A k step of 32 is one v_mfma_f32_16x16x32_bf16, both operands as they lie in memory; eight steps' loads on their way at a time.
-// grid: (heads, ceil(n / 64), ceil(m / 16))
+// grid: (heads, ceil(n / 64))
 __global__ void __launch_bounds__(256) k_head_product_few(HeadProductArgs a) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l15 = lane & 15, kg = lane >> 4;
-  const int h = blockIdx.x, n0 = blockIdx.y * 64 + wave * 16, m0 = blockIdx.z * 16;
+  const int h = blockIdx.x, n0 = blockIdx.y * 64 + wave * 16;
   if (n0 >= a.n) return;
-  const bf16_t* x = a.x + min(m0 + l15, a.m - 1) * a.x_row + h * a.x_head + kg * 8;
+  const bf16_t* x = a.x + min(l15, a.m - 1) * a.x_row + h * a.x_head + kg * 8;
   const bf16_t* w = a.w + ((size_t)h * a.n + n0 + l15) * a.k + kg * 8;
   f32x4_t acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
   int k = 0;
@@ -30,9 +34,9 @@ __global__ void __launch_bounds__(256) k_head_product_few(HeadProductArgs a) {
   if (k + 128 <= a.k) steps(xf, wf, 4);
   while (k < a.k) steps(xf, wf, 1);
   const f32x4_t y = acc[0] + acc[1];
-  // y[i]: column n0 + kg * 4 + i of row m0 + l15
-  if (m0 + l15 < a.m)
-    *reinterpret_cast<uint2*>(a.out + (m0 + l15) * a.out_row + h * a.out_head + n0 + kg * 4) = uint2{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
+  // y[i]: column n0 + kg * 4 + i of row l15
+  if (l15 < a.m)
+    *reinterpret_cast<uint2*>(a.out + l15 * a.out_row + h * a.out_head + n0 + kg * 4) = uint2{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
 }
 
 // ---- more: a workgroup has 64 rows x BN columns of a head -----------------------------------
@@ -104,8 +108,9 @@ __global__ void __launch_bounds__(256) k_head_product(HeadProductArgs a) {
 }
 
 hipError_t sp_launch_head_product(const HeadProductArgs& a, hipStream_t st) {
-  if (a.m <= 32) {
-    hipLaunchKernelGGL(k_head_product_few, dim3(a.heads, (a.n + 63) / 64, (a.m + 15) / 16), dim3(256), 0, st, a);
+  // Few rows, and a workgroup a CU at most (16 rows: 16 heads 128 -> 512 3.0 us, in blocks of 64 rows 3.3; 128 heads 5.9 and 4.3).
+  if (a.m <= 16 && (long long)a.heads * ((a.n + 63) / 64) <= 256) {
+    hipLaunchKernelGGL(k_head_product_few, dim3(a.heads, (a.n + 63) / 64), dim3(256), 0, st, a);
     return hipGetLastError();
   }
   // (blocks of rows in several launches where there are more than a grid takes)
@@ -115,7 +120,8 @@ hipError_t sp_launch_head_product(const HeadProductArgs& a, hipStream_t st) {
     b.out += m0 * a.out_row;
     b.m = (int)(a.m - m0 < 64 * 65535 ? a.m - m0 : 64 * 65535);
     const int blocks = (b.m + 63) / 64;
-    if (a.n > 64 && (long long)a.heads * blocks * ((a.n + 127) / 128) >= 256)
+    // 128 columns where that leaves two workgroups a CU (64 heads 512 -> 128: 640 rows 14.3 us, 64 columns 16.9; 256 rows 8.5 and 7.8)
+    if (a.n > 64 && (long long)a.heads * blocks * ((a.n + 127) / 128) >= 512)
       hipLaunchKernelGGL(k_head_product<128>, dim3(a.heads, (a.n + 127) / 128, blocks), dim3(256), 0, st, b);
     else
       hipLaunchKernelGGL(k_head_product<64>, dim3(a.heads, (a.n + 63) / 64, blocks), dim3(256), 0, st, b);

@@ -3,10 +3,12 @@
 // float32, bf16 or 4-bit values (sp_fp4.h).
 //
 //   q, k : y = x * rsqrt(mean(x^2) + eps) * gain over the head's columns (where the stage has head norms), then
-//          (a, b) -> (a cos - b sin, b cos + a sin) for the pairs (t, t + d_head / 2) at angle position * theta^(-2t / d_head)
+//          (a, b) -> (a cos - b sin, b cos + a sin) for the pairs (t, t + d_head / 2) at angle position * theta^(-2t / d_head);
+//          or, by sp_stage_set_rope, the pairs (t, t + dims / 2) or (2t, 2t + 1) of the first dims columns at given frequencies, times a gain
 //   v    : copied
 //
-// A head belongs to d_head / 8 consecutive lanes, a lane holds four pairs: columns t .. t+3 and d_head/2 + t .. + 3.  Sums over
+// A head belongs to d_head / 8 consecutive lanes, a lane holds four pairs: columns t .. t+3 and d_head/2 + t .. + 3, or eight columns in a
+// row, or columns that pass.  Sums over
 // the head and maxima over the eight lanes of a 4-bit group stay in the wave; nothing goes through LDS but the angles' sines.
 // Everything is float32 until the one rounding to the storage type.  Bound by the launch and a chain of lookups (request,
 // its prefix, the node's depth, its page) for a tree level: one row 3.6 us, 64 rows 4.2; 640 rows, 16 MB, 6.8.

@@ -3,7 +3,8 @@
 //
 //   latent : c * rsqrt(mean(c^2) + eps) * gain (where the stage has norms), key part and queries: rotated at prefix_len + depth
 //
-// Float32 until the one rounding to bf16; the angles in double precision, whole turns taken off there.
+// Float32 until the one rounding to bf16; the angles in double precision, whole turns taken off there.  The append is bound by its launch and
+// by the chain request -> node -> depth, slot, page: one row of 16 heads 3.6 us; 668 rows of 64 heads, 12 MB in and out, 5.9.
 #include "sp_launch.h"
 
 __device__ __forceinline__ void load8(const bf16_t* p, float (&v)[8]) {
@@ -139,7 +140,8 @@ hipError_t sp_launch_latent_rows(bool store, KvGeom g, int req, long long base, 
 
 // ---- tree attention, plain ----------------------------------------------------------
 // A workgroup has a (row, head): 256 slots at a time, a score a thread, then the weights meet the latents, columns over the threads.
-// (What the matrix-core kernel does not cover, and SP_FLAG_SIMPLE_KERNELS.)
+// (What the matrix-core kernel does not cover, and SP_FLAG_SIMPLE_KERNELS.  Each (row, head) reads the range for itself: 16 rows behind 512
+// slots 189 us, 80 behind 32749 11.6 ms.)
 #define LATENT_MAX 1024            // columns of a latent
 __global__ void __launch_bounds__(256) k_latent_attn_simple(LatentAttnArgs a, AttnPlan plan) {
   __shared__ float s_q[LATENT_MAX + 2 * SP_ROPE_PAIRS], s_p[256], s_red[4];

@@ -1,5 +1,25 @@
-#include <type_traits>
-
+// Tree attention over a latent cache on the matrix cores: d_latent 256 and 512, d_rope 32 and 64.
+//
+//   out = softmax(scale * q . [c | r]) c     over the rows [c | r] of the cache that the node sees (committed context, ancestors, itself)
+//
+// The cache has one row a slot for all heads, so the nodes and heads of a request are the rows of one matrix, node * heads + head, and
+// a workgroup takes 32 or 64 of them along a chunk of the request's range: 2 (2 d_latent + d_rope) operations a row and slot stand
+// against the slot's (d_latent + d_rope) * 2 bytes.  Tiles of 32 slots lie in LDS as they lie in the cache and are used from there twice:
+// rows of them for the scores (16x16x32), columns of them, by the transposing reads, for the results (32x32x16).  The 64 x 512 float32
+// results fill the registers of four waves; the other four form the scores, weights and row sums, a tile ahead, so that every SIMD has a
+// wave of either kind and one's products pass behind the other's LDS reads and exponentials (eight waves that did both in turn: 118 us a
+// call, this way 93).  Four tiles are in LDS: two on their way, one under the scores, one under the results; one barrier a tile.
+//
+// Running softmax with a shift that hardly ever moves: a row's weights are exp2 of its score less a past maximum, and only where a tile
+// has weights past 2^16 are its maxima taken, the row's results scaled, and the tile taken again.  Weights are rounded to bf16 (2^-8 of
+// each at most), and the row's sum is that of the rounded ones, so that what rounding adds to numerator and denominator is the same; all
+// else is float32.  Chunks leave unnormalized results, sums and shifts, which k_latent_merge_few and k_latent_merge join.
+//
+// Bound by LDS and the clock under full load (1.75 to 1.83 of 2.4 GHz): a tile of 64 rows takes 1736 cycles where its reads (scores 576 and 160,
+// results 256) and the rows coming in (288) need 1280 at 128 bytes a clock and its products 1088.  A workgroup has 4.5 us beside its
+// tiles (first rows, query rows, results out).  512 + 64 columns: 128 nodes x 64 heads behind 4096 slots 71 us, 1.05 PFLOP/s (a large
+// library product 1.41), and 8.7 of merge; 64 x 32 behind 2048 21.8 and 4.4; 16 rows behind 512
+// 8.7 and 3.5.
 #include "sp_latent_plan.h"
 #include "sp_launch.h"
 
@@ -407,12 +427,14 @@ __device__ __forceinline__ LatentRow latent_row(const AttnPlan& plan, int at, in
   return {plan.seg_chunks[seg], (size_t)plan.seg_unit0[seg] + at - (size_t)plan.seg_row0[seg] * H, (size_t)plan.seg_rows[seg] * H};
 }
 
-// Few chunks: a wave joins those of a query row, DC / 64 columns a lane, four chunks on their way at a time.
+// Chunks j of a row, results o_j, sums l_j, shifts m_j: out = sum_j w_j o_j / sum_j w_j l_j with w_j = exp2(m_j - max m).  Bound by the
+// partial rows' way in.  Few chunks: a wave joins those of a query row, DC / 64 columns a lane, four chunks on their way at a time (8192
+// rows of two chunks 8.7 us, 33 MB; the 16 to 128 rows of 32 requests in up to four 5.4; with the kernel for many 19.6 and 9.3).
 #define LATENT_FEW 16
 template <int DC>
-__global__ void __launch_bounds__(256) k_latent_merge_few(LatentAttnArgs a, AttnPlan plan, int n) {
+__global__ void __launch_bounds__(256) k_latent_merge_few(LatentAttnArgs a, AttnPlan plan, int at0, int n) {
   constexpr int V = DC / 256;                      // four columns at lane * 4 + 256 v
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, at = blockIdx.x * 4 + wave;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, at = at0 + blockIdx.x * 4 + wave;
   if (at >= n) return;
   const LatentRow r = latent_row(plan, at, a.d.n_heads, lane);
   if (r.chunks == 1) return;
@@ -449,13 +471,13 @@ __global__ void __launch_bounds__(256) k_latent_merge_few(LatentAttnArgs a, Attn
 }
 
 // Many: a workgroup joins those of a query row, a thread four columns, groups of threads every second chunk (DC 256: fourth), eight on
-// their way at a time.
+// their way at a time (80 rows of 64 chunks 5.2 us; with the kernel for few 14.4).
 template <int DC>
-__global__ void __launch_bounds__(256) k_latent_merge(LatentAttnArgs a, AttnPlan plan) {
+__global__ void __launch_bounds__(256) k_latent_merge(LatentAttnArgs a, AttnPlan plan, int at0) {
   constexpr int T = DC / 4, G = 256 / T;           // threads of a row, groups of chunks
   __shared__ float s_w[256], s_red[8];
   __shared__ __attribute__((aligned(16))) float s_acc[(G - 1) * DC];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, at = blockIdx.x;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, at = at0 + blockIdx.x;
   const LatentRow r = latent_row(plan, at, a.d.n_heads, lane);
   if (r.chunks == 1) return;
   const int chunks = r.chunks;
@@ -516,9 +538,15 @@ static hipError_t go(const LatentAttnArgs& a, const AttnPlan& plan, int M, hipSt
   const int n = M * a.d.n_heads;
   int most = 0;
   for (int i = 0; i < plan.n_seg; ++i) most = plan.seg_chunks[i] > most ? plan.seg_chunks[i] : most;
-  if (most <= LATENT_FEW) hipLaunchKernelGGL((k_latent_merge_few<DC>), dim3((n + 3) / 4), dim3(256), 0, st, a, plan, n);
-  else hipLaunchKernelGGL((k_latent_merge<DC>), dim3(n), dim3(256), 0, st, a, plan);
-  return hipGetLastError();
+  // (in several launches where there are more query rows than a grid takes)
+  for (int at0 = 0; at0 < n; at0 += 1 << 23) {
+    const int rows = n - at0 < 1 << 23 ? n - at0 : 1 << 23;
+    if (most <= LATENT_FEW) hipLaunchKernelGGL((k_latent_merge_few<DC>), dim3((rows + 3) / 4), dim3(256), 0, st, a, plan, at0, n);
+    else hipLaunchKernelGGL((k_latent_merge<DC>), dim3(rows), dim3(256), 0, st, a, plan, at0);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 template <int DC, int DR>
 static hipError_t go(const LatentAttnArgs& a, const AttnPlan& plan, int M, hipStream_t st) {

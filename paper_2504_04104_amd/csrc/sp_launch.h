@@ -213,10 +213,11 @@ struct RotateArgs {
   long long x_row, x_head, out_row, out_head;
   const int* pos;                  // [n_rows]
   int n_rows, n_heads, d_head, dims, layout;
+  int rows_per;                    // rows of a workgroup, made at the launch
   float gain, sign;                // sign -1: back
   double freq[2 * SP_ROPE_PAIRS];
 };
-hipError_t sp_launch_rotate(int dtype, const RotateArgs& a, hipStream_t st);
+hipError_t sp_launch_rotate(int dtype, RotateArgs& a, hipStream_t st);
 
 // ---- latent cache: one row of d_latent + d_rope bf16 values a token and layer ---------
 struct LatentDims { int n_heads, d_latent, d_rope; };

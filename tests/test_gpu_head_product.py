@@ -88,3 +88,11 @@ def test_refusals():
     refused(-9, lambda: sp.head_product(x, w, out=torch.zeros(4, 1, 32, dtype=torch.bfloat16, device="cuda").expand(4, 2, 32)))
     refused(-9, lambda: sp.head_product(rnd(1, 4, 2, 68)[..., :64], w))
     assert sp.head_product(x[:0], w).shape == (0, 2, 32)
+
+
+@pytest.mark.parametrize("heads,n,k", [(16, 512, 128), (33, 512, 128), (64, 128, 512), (128, 64, 96)])
+@pytest.mark.parametrize("m", [1, 16, 17, 64, 65, 256, 449])
+def test_few_heads_and_many(m, heads, n, k):
+    """Either side of where the rows of a block and the columns of a workgroup change."""
+    x, w = rnd(m, m, heads, k), rnd(n, heads, n, k, scale=k ** -0.5)
+    near(sp.head_product(x, w), x, w)

@@ -242,3 +242,30 @@ def test_refusals():
     refused(-9, lambda: st.set_rope(sp.Rope("half", 32, 10000.0)))
     refused(-1, lambda: st.set_rope(sp.Rope("half", 256, 10000.0)))
     assert sp.rotate(x[:0], pos[:0], rope).shape == (0, 2, 64)
+
+
+def test_more_rows_than_a_launch_takes():
+    """The rows behind the 2^23rd, in either layout and with a head of its own stride, as a call of them alone turns them."""
+    n, tail = 2 ** 23 + 77, 100
+    x = torch.zeros(n, 1, 16, dtype=torch.bfloat16, device="cuda")
+    x[-tail:] = rows(3, tail, 1, 16)
+    x[:50] = x[-50:]
+    pos = torch.arange(n, dtype=torch.int32, device="cuda")
+    for layout in ("half", "interleaved"):
+        rope = sp.Rope(layout, 8, 10000.0)
+        got = sp.rotate(x, pos, rope)
+        assert torch.equal(got[-tail:], sp.rotate(x[-tail:].contiguous(), pos[-tail:].contiguous(), rope))
+        assert torch.equal(got[:50], sp.rotate(x[:50].contiguous(), pos[:50].contiguous(), rope))
+        assert not got[50:-tail].any()
+
+
+@pytest.mark.parametrize("heads", [1, 4, 8, 31, 32, 33, 64])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_rows_that_share_a_workgroup(heads, dtype):
+    """Whatever the number of rows that a workgroup takes: a call of many rows has the bits of calls of one."""
+    x = rows(heads, 19, heads, 128, dtype=dtype)
+    pos = torch.arange(19, dtype=torch.int32, device="cuda") * 1777
+    rope = sp.Rope("interleaved", 64, 10000.0)
+    got = sp.rotate(x, pos, rope)
+    for i in range(19):
+        assert torch.equal(got[i:i + 1], sp.rotate(x[i:i + 1], pos[i:i + 1], rope))
