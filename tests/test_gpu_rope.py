@@ -194,6 +194,28 @@ def test_forward_rotates_as_the_pieces_do(dtype, n, kind):
         assert np.median(np.abs(f64(k) - want)) <= 4 * u * np.median(np.abs(want))
 
 
+@pytest.mark.parametrize("n", [3, 40, 200])
+@pytest.mark.parametrize("kind", ["part", "interleaved"])
+def test_forward_into_a_cache_of_4_bits(n, kind):
+    """Beside a bf16 cache's: the same float32 keys rounded to 4 bits and to bf16.  bf16's half step of 2^-9 of a value on average, and
+    2^-8 at most, puts a value across a border between codes, which lie v / 4 apart or wider, for at most 2 * 2^-8 * 4 = 3.1 % of them, and a group's
+    largest across a power of two for 2 * 2^-8 * 1.44 = 1.1 %."""
+    from fp4_reference import held
+    use_own_stream()
+    sh = wl.ModelShape(1, 512, 4, 2, 128, 512, 1e-5, 500000.0, "bf16")
+    rope = sp.Rope("half", 64, 10000.0) if kind == "part" else sp.Rope("interleaved", 128, 10000.0, SCALINGS[1])
+    keys, layers = [], None
+    for flags in (0, sp.SP_FLAG_FP4_KV):
+        st = stage(sp, sh, slots=1024, rows=256, flags=flags, layers=layers)
+        layers = st.plain_layers
+        st.request_init(0, 0, 900, 300)
+        st.tree_insert(0, [-1] * n)
+        st.set_rope(rope)
+        st.stage_forward([0], [0], [n], rows(7, n, 512))
+        keys.append(f64(st.kv_load(0, 0, 300, n)[0]))
+    assert (keys[1] == held(keys[0])).mean() >= 1 - 0.031 - 0.011
+
+
 def test_replayed_forward_calls_take_a_new_rotation():
     """Layers enough that calls are replayed: a rotation that is set between them is that of the next call."""
     use_own_stream()
