@@ -418,13 +418,18 @@ int sp_latent_query_sizes(const sp_config* cfg, const sp_latent* latent, sp_size
   return SP_OK;
 }
 
-// What every stage has: buffers, tables, pages, the device.  sz: what the buffers have to hold at least.
-static int make_stage(const sp_config* cfg, const sp_sizes& sz, const sp_buffers* buffers, sp_stage** out) {
+// sz: what the buffers have to hold at least.
+static int check_buffers(const sp_sizes& sz, const sp_buffers* buffers) {
   if (!buffers->kv || !buffers->tables || !buffers->workspace) return SP_E_INVALID;
   if (buffers->kv_bytes < sz.kv_bytes || buffers->tables_bytes < sz.tables_bytes ||
       buffers->workspace_bytes < sz.workspace_bytes)
     return SP_E_CAPACITY;
   if (((uintptr_t)buffers->kv | (uintptr_t)buffers->tables | (uintptr_t)buffers->workspace) & 255) return SP_E_INVALID;
+  return SP_OK;
+}
+
+// What every stage has: buffers, tables, pages, the device.
+static int make_stage(const sp_config* cfg, const sp_sizes& sz, const sp_buffers* buffers, sp_stage** out) {
   int dev = 0, cus = 0;
   if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= SP_NOALLOC_MAX_DEVICES) return SP_E_HIP;
   if (!g_noalloc_scratch[dev]) {
@@ -476,16 +481,14 @@ int sp_stage_create(const sp_config* cfg, const sp_layer_weights* layers, const 
   if (!layers || !buffers || !out) return SP_E_INVALID;
   sp_sizes sz;
   sp_stage_query_sizes(cfg, &sz);
-  sp_stage* s = nullptr;
-  if ((rc = make_stage(cfg, sz, buffers, &s)) != SP_OK) return rc;
+  if ((rc = check_buffers(sz, buffers)) != SP_OK) return rc;
   for (int l = 0; l < cfg->n_layers; ++l) {
     const sp_layer_weights& w = layers[l];
-    if (!w.wqkv || !w.wo || !w.wgu || !w.wd || !w.norm1 || !w.norm2 ||
-        (((uintptr_t)w.wqkv | (uintptr_t)w.wo | (uintptr_t)w.wgu | (uintptr_t)w.wd) & 15)) {
-      delete s;
-      return SP_E_INVALID;
-    }
+    if (!w.wqkv || !w.wo || !w.wgu || !w.wd || !w.norm1 || !w.norm2) return SP_E_INVALID;
+    if (((uintptr_t)w.wqkv | (uintptr_t)w.wo | (uintptr_t)w.wgu | (uintptr_t)w.wd) & 15) return SP_E_INVALID;
   }
+  sp_stage* s = nullptr;
+  if ((rc = make_stage(cfg, sz, buffers, &s)) != SP_OK) return rc;
   s->W.assign(layers, layers + cfg->n_layers);
   s->ws = carve(*cfg, (char*)buffers->workspace);
   s->geom.scale_plane_bytes = scale_plane_bytes(*cfg);
@@ -511,6 +514,7 @@ int sp_latent_stage_create(const sp_config* cfg, const sp_latent* latent, const 
   if (!buffers || !out) return SP_E_INVALID;
   sp_sizes sz;
   sp_latent_query_sizes(cfg, latent, &sz);
+  if ((rc = check_buffers(sz, buffers)) != SP_OK) return rc;
   sp_stage* s = nullptr;
   if ((rc = make_stage(cfg, sz, buffers, &s)) != SP_OK) return rc;
   s->latent = true;

@@ -79,7 +79,7 @@ def test_refused_rotations():
     for bad in (dict(dtype=2), dict(inverse=2), dict(x=None), dict(x=ODD), dict(rows=-1), dict(heads=0), dict(d=0), dict(pos=None), dict(pos=C.c_void_p(4098)), dict(out=None),
                 dict(out=ODD), dict(out=P[0], out_row=256), dict(out=C.c_void_p(P[0].value + 128)), dict(pos=P[2]), dict(pos=C.c_void_p(P[2].value + 500))):
         assert call(**bad) == INVALID, bad
-    for bad in (dict(d=68), dict(d=264), dict(x_row=-8), dict(x_head=4), dict(x_row=1 << 31), dict(out_row=64), dict(out_head=0), dict(out_head=32), dict(out_row=0),
+    for bad in (dict(d=68), dict(d=264), dict(heads=65537, x_head=0, out_head=64, out_row=65537 * 64), dict(x_row=-8), dict(x_head=4), dict(x_row=1 << 31), dict(out_row=64), dict(out_head=0), dict(out_head=32), dict(out_row=0),
                 dict(out_row=100)):
         assert call(**bad) == UNSUPPORTED, bad
     assert lib.sp_rotate(None, *good.values(), None) == INVALID
@@ -122,3 +122,31 @@ def test_calls_without_a_stage():
 def test_struct_layouts():
     assert C.sizeof(binding.sp_rope) == 16 + 8 * 128 and binding.sp_rope.freq.offset == 16
     assert C.sizeof(binding.sp_latent) == 24 and binding.sp_latent.norms.offset == 16
+
+
+def test_stages_that_are_refused_before_the_device_is_asked():
+    """Buffers too small or out of line, weights that are none: the same answers with and without a GPU."""
+    lib = sp.load_library()
+    out = C.c_void_p()
+    cfg = binding.sp_config(1, 256, 4, 1, 576, 8, 1e-5, 10000.0, binding.SP_BF16, 1, 256, 16, 256, 0, 0)
+    lat, sz = binding.sp_latent(512, 64, 0.1, 0, None), binding.sp_sizes()
+    assert lib.sp_latent_query_sizes(C.byref(cfg), C.byref(lat), C.byref(sz)) == OK
+    plain = binding.sp_config(1, 256, 2, 1, 128, 256, 1e-5, 10000.0, binding.SP_BF16, 1, 256, 16, 256, 0, 0)
+    psz = binding.sp_sizes()
+    assert lib.sp_stage_query_sizes(C.byref(plain), C.byref(psz)) == OK
+    weights = (binding.sp_layer_weights * 1)()
+
+    def create(latent, **kw):
+        z = sz if latent else psz
+        b = dict(kv=P[0], kv_bytes=z.kv_bytes, tables=P[1], tables_bytes=z.tables_bytes, workspace=P[2], workspace_bytes=z.workspace_bytes)
+        bufs = binding.sp_buffers(*{**b, **kw}.values())
+        if latent:
+            return lib.sp_latent_stage_create(C.byref(cfg), C.byref(lat), C.byref(bufs), None, C.byref(out))
+        return lib.sp_stage_create(C.byref(plain), weights, C.byref(bufs), None, C.byref(out))
+    for latent in (True, False):
+        for bad in (dict(kv=None), dict(tables=None), dict(workspace=None), dict(kv=ODD), dict(tables=ODD), dict(workspace=ODD)):
+            assert create(latent, **bad) == INVALID, bad
+        for bad in (dict(kv_bytes=8), dict(tables_bytes=8), dict(workspace_bytes=8)):
+            assert create(latent, **bad) == -2, bad
+    assert create(False) == INVALID                                     # (weights that are none)
+    assert out.value is None
