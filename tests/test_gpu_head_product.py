@@ -96,3 +96,25 @@ def test_few_heads_and_many(m, heads, n, k):
     """Either side of where the rows of a block and the columns of a workgroup change."""
     x, w = rnd(m, m, heads, k), rnd(n, heads, n, k, scale=k ** -0.5)
     near(sp.head_product(x, w), x, w)
+
+
+@pytest.mark.parametrize("heads,n,k", [(40, 320, 64), (64, 64, 64), (24, 512, 128), (48, 192, 128), (32, 192, 192), (16, 1024, 256)])
+@pytest.mark.parametrize("m", [97, 641, 2049])
+def test_columns_kept_for_many_rows(m, heads, n, k):
+    """Columns that end inside a workgroup, rows inside a block; workgroups with one block and with more."""
+    x, w = rnd(m, m, heads, k), rnd(n, heads, n, k, scale=k ** -0.5)
+    near(sp.head_product(x, w), x, w)
+
+
+@pytest.mark.parametrize("k", [64, 128, 192, 256])
+def test_views_of_many_rows(k):
+    m, heads, n = 1100, 32, 320
+    q, w = rnd(1, m + 1, heads, k + 24), rnd(2, heads, n, k, scale=0.1)
+    wide = torch.full((m + 1, heads, n + 40), 3.0, dtype=torch.bfloat16, device="cuda")
+    sp.head_product(q[:m, :, 8:k + 8], w, out=wide[:m, :, 8:n + 8])
+    near(wide[:m, :, 8:n + 8], q[:m, :, 8:k + 8], w)
+    assert (wide[m] == 3).all() and (wide[..., :8] == 3).all() and (wide[..., n + 8:] == 3).all()
+    one = q[:1, :, :k].expand(m, heads, k)
+    got = sp.head_product(one, w)
+    assert torch.equal(got, got[:1].expand(m, heads, n))
+    near(got[:1], one[:1], w)
