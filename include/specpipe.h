@@ -368,7 +368,7 @@ int sp_latent_append(sp_stage* stage, int32_t layer, int32_t n_req, const int32_
  * d_rope], out [sum n_nodes][n_q_heads][d_latent] = softmax(scale * q . row) over the rows of the committed context, the node itself and
  * its ancestors, times those rows' latents.  Sums and softmax statistics are float32; the softmax's weights are rounded to bf16 before
  * they meet the latents, and divided by the sum of the rounded ones.  q and out are 16-byte aligned device memory and may not overlap.
- * Uses the stage's workspace. */
+ * Uses the stage's workspace.  A call that the caller captures keeps the trees' sizes and prefix lengths of then. */
 int sp_latent_attention(sp_stage* stage, int32_t layer, int32_t n_req, const int32_t* req_ids /*host*/,
                         const int32_t* first_node /*host*/, const int32_t* n_nodes /*host*/, const void* q, void* out, sp_stream stream);
 

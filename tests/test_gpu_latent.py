@@ -361,6 +361,22 @@ def test_captured_pieces_replay_with_the_values_of_the_time():
         check_rows(got, q2, st.kv_load(0, 0, 0, 2009), c, seen_by(st, 0), (c // 4 + r) ** -0.5)
 
 
+@pytest.mark.parametrize("page", [0, 64])
+def test_requests_without_nodes_in_a_call(page):
+    """They are passed over: the others' bits, cache rows and what counts as forwarded are those of a call without them."""
+    trees = [(70, 3), (500, 4), (9, 2), (1300, 1)]
+    got = []
+    for ids in ([0, 1, 2, 3], [0, 2, 3]):
+        st = make(16, 512, 64, trees, page=page, seed=3)
+        n = [trees[i][1] if i != 1 else 0 for i in ids]
+        q, kv = rnd(5, 6, 16, 576), rnd(6, 6, 576)
+        st.append(0, ids, [0] * len(ids), n, q[..., 512:], kv, q[..., 512:])
+        y = st.attention(0, ids, [0] * len(ids), n, q)
+        got.append((q, y, torch.cat([st.kv_load(i, 0, 0, P + T) for i, (P, T) in enumerate(trees)])))
+        assert [st.request_info(i)[2] for i in range(4)] == [3, 0, 2, 1]
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
 def test_two_stages_on_two_streams_and_repeated_calls():
     """Calls that overlap in time on stages of their own, and the same call over and over: equal bits."""
     sts = [make(16, 512, 64, [(6000, 3)], seed=s) for s in (1, 2)]
