@@ -46,6 +46,19 @@ __device__ __forceinline__ float dot2(uint32_t w, float acc) {
 }
 __device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u; }
 
+// Sums over the lanes up to one's own.
+__device__ __forceinline__ int wave_scan(int v) {
+#ifdef __HIP_DEVICE_COMPILE__
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);         // from 1, 2, 4 and 8 lanes below in rows of 16
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, true);         // a row's last lane to the second and fourth
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, true);         // the second row's to the upper half
+#endif
+  return v;
+}
+
 #define LW 8                       // waves per workgroup: four form scores, four the results
 #define LK 32                      // slots per tile
 
@@ -72,14 +85,27 @@ __global__ void __launch_bounds__(64 * LW, 2) k_latent_attn(LatentAttnArgs a, At
   auto uni = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
   const int wave = uni((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int l15 = lane & 15, kg = lane >> 4;
-  const int item = blockIdx.x;
-  int seg = 0;
-  if (plan.n_seg > 1) seg = uni(__popcll(__builtin_amdgcn_ballot_w64(lane < plan.n_seg && item >= plan.seg_item0[lane])) - 1);
+  const int xcd = blockIdx.x & 7;
+  int seg = 0, local = blockIdx.x >> 3;            // the workgroup's request, and its number among the request's on this XCD
+  if (plan.n_seg > 1) {
+    int n = 0;
+    if (lane < plan.n_seg) {
+      const LatentPlace p = latent_unpack(plan.seg_item0[lane]);
+      n = latent_units_on(plan.seg_chunks[lane] * p.groups, p.start, xcd) * p.group;
+    }
+    const int to = wave_scan(n);                   // workgroups of the requests up to the lane's
+    seg = uni(__popcll(__builtin_amdgcn_ballot_w64(lane < plan.n_seg && to <= local)));
+    if (seg >= plan.n_seg) return;
+    local -= __builtin_amdgcn_readlane(to - n, seg);
+  }
+  const LatentPlace place = latent_unpack(plan.seg_item0[seg]);
+  // (quotients of numbers below 2^21 by way of float32: half a step of the quotient is more than they are off)
+  const int group = place.group, groups = place.groups, nth = uni((int)(((float)local + 0.5f) * __builtin_amdgcn_rcpf((float)group)));
+  const int unit = latent_first(place.start, xcd) + nth * 8;
   const int chunks = plan.seg_chunks[seg], seg_rows = plan.seg_rows[seg], row0 = plan.seg_row0[seg], req = plan.seg_req[seg];
   const int P = plan.seg_P[seg], span = P + plan.seg_T[seg], clen = plan.seg_clen[seg];
-  const LatentItem work = latent_item(item - plan.seg_item0[seg], plan.seg_qblocks[seg], chunks);
-  const int qb = uni(work.block), ch = uni(work.chunk);
-  if (ch >= chunks) return;
+  const int ch = uni((int)(((float)unit + 0.5f) * __builtin_amdgcn_rcpf((float)groups))), qb = unit - ch * groups + (local - nth * group) * groups;
+  if (ch >= chunks || qb >= plan.seg_qblocks[seg]) return;
   const int H = a.d.n_heads, nq = seg_rows * H;    // query rows of the request, node * H + head
   const int c0 = ch * clen, c1 = min(c0 + clen, span), tiles = (c1 - c0 + LK - 1) / LK;
 

@@ -3,40 +3,79 @@
 #include "sp_plan.h"
 
 #define LATENT_TILE 64             // slots that a workgroup takes at a time
+#define LATENT_FAR (16 << 20)      // bytes of latents that a call reads from where they do not stay in L2
 
-// Workgroups of a request, (block of query rows, chunk) by number: chunk after chunk for every block, or, where there are eight chunks and
-// more, eight chunks side by side for every block, so that a chunk's blocks run on the XCD whose L2 has it (consecutive workgroups go
-// round over the eight; 80 rows behind 32749 slots in 64 chunks 24.7 us, in 74, which scattered them, 30.3).  The last eight chunks
-// may be part empty: chunk >= chunks then, nothing to do.
-struct LatentItem { int block, chunk; };
+// Workgroups of a call.  Consecutive ones go round over the eight XCDs: workgroup i is number i / 8 of those of XCD i % 8.  A request's work is
+// cut into units, a chunk and `group` of its blocks of query rows, every groups-th from one on (some may be short: workgroups without a
+// block), which follow each other over the XCDs from `start` on, request after request: the blocks of a unit read the same rows at the same
+// time behind the same L2.
+struct LatentPlace { int group, groups, start; };           // (blocks are at most 8192: 256 nodes x 1024 heads in blocks of 32)
 #ifdef __HIPCC__
-__host__ __device__
+#define LATENT_BOTH __host__ __device__
+#else
+#define LATENT_BOTH
 #endif
-inline LatentItem latent_item(int local, int blocks, int chunks) {
-  if (chunks < 8 || blocks == 1) return {local / chunks, local % chunks};
-  const int eights = local >> 3;
-  return {eights % blocks, eights / blocks * 8 + (local & 7)};
+inline int latent_pack(LatentPlace p) { return p.groups << 17 | p.group << 3 | p.start; }
+LATENT_BOTH inline LatentPlace latent_unpack(int v) { return {(v >> 3) & 0x3fff, v >> 17, v & 7}; }
+// The request's first unit on XCD x, and how many it has there.
+LATENT_BOTH inline int latent_first(int start, int x) { return (x - start) & 7; }
+LATENT_BOTH inline int latent_units_on(int units, int start, int x) {
+  const int j = latent_first(start, x);
+  return j < units ? ((units - 1 - j) >> 3) + 1 : 0;
 }
-inline int latent_items(int blocks, int chunks) { return (chunks < 8 || blocks == 1 ? chunks : (chunks + 7) / 8 * 8) * blocks; }
+
+// Groups of up to `most` blocks; returns the longest row of workgroups of an XCD.
+inline int latent_place(AttnPlan& plan, int most) {
+  int load[8] = {0, 0, 0, 0, 0, 0, 0, 0}, start = 0, longest = 0, grid = 0;
+  for (int i = 0; i < plan.n_seg; ++i) {
+    const int blocks = plan.seg_qblocks[i], cut = (blocks + most - 1) / most, group = (blocks + cut - 1) / cut, groups = (blocks + group - 1) / group;
+    const int units = plan.seg_chunks[i] * groups;
+    plan.seg_item0[i] = latent_pack({group, groups, start});
+    for (int x = 0; x < 8; ++x) load[x] += latent_units_on(units, start, x) * group;
+    start = (start + units) & 7;
+  }
+  for (int x = 0; x < 8; ++x) {
+    longest = load[x] > longest ? load[x] : longest;
+    if (load[x] > 0 && (load[x] - 1) * 8 + x + 1 > grid) grid = (load[x] - 1) * 8 + x + 1;
+  }
+  plan.total_items = grid;
+  return longest;
+}
+// Groups of up to four blocks where the rows that the call reads are too many for the L2s, 4 MB each, to have a chunk when it is asked for
+// again, and the XCDs stay nearly level (32 requests of 1 to 8 nodes x 16 heads, 75 MB: 33.2 us, 36.6 one by one; 80 query rows behind 32749 slots
+// 26.5 and 29.9); else one by one (64 nodes x 32 heads behind 2048, 2 MB: 28.1, in groups of 32 30.0; 8 requests of 1 to 2 nodes x 128 heads, 6 MB:
+// 22.5 in blocks of 64, in groups 24.2).
+inline void latent_place(AttnPlan& plan, long long items, int n_cu, long long bytes) {
+  int most = 1;
+  if (bytes > LATENT_FAR)
+    for (int i = 0; i < plan.n_seg; ++i) most = plan.seg_qblocks[i] > most ? plan.seg_qblocks[i] : most;
+  if (most > 4) most = 4;
+  const long long share = (items + 7) / 8, per = n_cu / 8;
+  long long allowed = share + (share < 8 ? 1 : share / 8);
+  if (share <= per && allowed > per) allowed = per;
+  while (latent_place(plan, most) > allowed && most > 1) --most;
+}
 
 // Every request's range in chunks of at most `len` tiles, blocks of `rows` query rows; returns the partial rows that this takes.
-inline size_t latent_cut(AttnPlan& plan, int H, int rows, int len) {
+inline size_t latent_cut(AttnPlan& plan, int H, int d_latent, int rows, int len, int n_cu) {
   size_t units = 0;
-  int items = 0, split = 0;
+  long long items = 0, slots = 0;
+  int split = 0;
   plan.qt = rows / 16;
   for (int i = 0; i < plan.n_seg; ++i) {
     const int span = plan.seg_P[i] + plan.seg_T[i], tiles = (span + LATENT_TILE - 1) / LATENT_TILE;
     const int want = (tiles + len - 1) / len, each = (tiles + want - 1) / want, chunks = (tiles + each - 1) / each;
     const int qblocks = (int)(((long long)plan.seg_rows[i] * H + rows - 1) / rows);
-    plan.seg_item0[i] = items; plan.seg_chunks[i] = chunks; plan.seg_clen[i] = each * LATENT_TILE; plan.seg_qblocks[i] = qblocks;
+    plan.seg_chunks[i] = chunks; plan.seg_clen[i] = each * LATENT_TILE; plan.seg_qblocks[i] = qblocks;
     plan.seg_unit0[i] = (int)units;
-    items += latent_items(qblocks, chunks);
+    items += (long long)qblocks * chunks;
+    slots += span;
     if (chunks > 1) { units += (size_t)chunks * plan.seg_rows[i] * H; split = 1; }
   }
-  plan.total_items = items;
   plan.units_total = (int)units;
   plan.any_split = split;
   plan.loads = ATTN_SHARED;
+  latent_place(plan, items, n_cu, slots * d_latent * 2);
   return units;
 }
 
@@ -82,5 +121,5 @@ inline bool latent_split(AttnPlan& plan, int H, int d_latent, int n_cu, size_t r
       if (rounds > 4.) break;                      // (shorter chunks: more of everything but the last one's time)
     }
   }
-  return latent_cut(plan, H, best_rows, best_len) <= room;
+  return latent_cut(plan, H, d_latent, best_rows, best_len, n_cu) <= room;
 }

@@ -25,11 +25,9 @@ extern "C" int split(int n, const int* rows, const int* spans, int heads, int d_
   }
   return 1;
 }
-extern "C" void item(int local, int blocks, int chunks, int* block, int* chunk) {
-  const LatentItem w = latent_item(local, blocks, chunks);
-  *block = w.block; *chunk = w.chunk;
-}
-extern "C" int items(int blocks, int chunks) { return latent_items(blocks, chunks); }
+extern "C" void unpack(int v, int* group, int* groups, int* start) { const LatentPlace p = latent_unpack(v); *group = p.group; *groups = p.groups; *start = p.start; }
+extern "C" int first_of(int start, int x) { return latent_first(start, x); }
+extern "C" int units_on(int units, int start, int x) { return latent_units_on(units, start, x); }
 """
 
 
@@ -52,48 +50,90 @@ def split(lib, rows, spans, heads, d_latent=512, n_cu=256, room=40960):
     return out
 
 
-def test_every_plan_covers_its_ranges(lib):
-    """Chunks are whole tiles, none is empty, they cover the range; blocks cover the query rows; items and partial rows of the requests
-    follow each other; the partial rows fit the room, and no call is refused (a chunk each needs none)."""
-    r = random.Random(2)
-    for _ in range(3000):
+def placed(lib, v):
+    group, groups, start = C.c_int(), C.c_int(), C.c_int()
+    lib.unpack(v, C.byref(group), C.byref(groups), C.byref(start))
+    return group.value, groups.value, start.value
+
+
+def workgroups(lib, p):
+    """(request, block, chunk) of every workgroup, None for those without, found as the kernel finds them."""
+    segs = []
+    for v, chunks, _, blocks, _ in p["segs"]:
+        group, groups, start = placed(lib, v)
+        assert groups == -(-blocks // group) and 0 <= start < 8
+        segs.append((group, start, groups, chunks, blocks))
+    out = []
+    for i in range(p["items"]):
+        x, local, work = i % 8, i // 8, None
+        for seg, (group, start, groups, chunks, blocks) in enumerate(segs):
+            n = lib.units_on(chunks * groups, start, x) * group
+            if local < n:
+                unit = lib.first_of(start, x) + local // group * 8
+                chunk, block = unit // groups, unit % groups + local % group * groups
+                assert chunk < chunks
+                work = (seg, block, chunk) if block < blocks else None
+                break
+            local -= n
+        out.append(work)
+    return out
+
+
+def random_calls(n, seed):
+    r = random.Random(seed)
+    for _ in range(n):
         heads = r.choice([1, 3, 8, 16, 64, 128, 1024])
         rows = [r.choice([1, 2, 5, 17, 64, 256]) for _ in range(r.choice([1, 1, 2, 5, 31, 64]))]
         spans = [v + int(2 ** r.uniform(0, r.choice([8, 15, 20]))) for v in rows]
-        room = r.choice([0, 2000, 40960])
-        p = split(lib, rows, spans, heads, r.choice([256, 512]), r.choice([32, 256]), room)
+        yield rows, spans, heads, r.choice([256, 512]), r.choice([32, 256]), r.choice([0, 2000, 40960])
+
+
+def test_every_plan_covers_its_ranges(lib):
+    """Chunks are whole tiles, none is empty, they cover the range; blocks cover the query rows; the requests' partial rows follow each
+    other; they fit the room, and no call is refused (a chunk each needs none)."""
+    for rows, spans, heads, d_latent, n_cu, room in random_calls(2000, 2):
+        p = split(lib, rows, spans, heads, d_latent, n_cu, room)
         assert p["qt"] in (2, 4)
-        item, unit, any_split = 0, 0, 0
-        for (item0, chunks, clen, qblocks, unit0), m, span in zip(p["segs"], rows, spans):
+        unit, any_split = 0, 0
+        for (_, chunks, clen, qblocks, unit0), m, span in zip(p["segs"], rows, spans):
             assert clen % 64 == 0 and (chunks - 1) * clen < span <= chunks * clen
             assert qblocks == -(-m * heads // (16 * p["qt"]))
-            assert (item0, unit0) == (item, unit)
-            item += lib.items(qblocks, chunks)
+            assert unit0 == unit
             unit += chunks * m * heads if chunks > 1 else 0
             any_split |= chunks > 1
-        assert (item, unit, any_split) == (p["items"], p["units"], p["any_split"])
+        assert (unit, any_split) == (p["units"], p["any_split"])
         assert unit <= room
 
 
 def test_every_block_and_chunk_has_one_workgroup(lib):
-    """Workgroups without a chunk are fewer than eight a block; a chunk's workgroups go to one XCD (the same number modulo eight) where
-    there are eight chunks and more."""
-    b, c = C.c_int(), C.c_int()
-    for blocks in (1, 2, 3, 5, 16, 31):
-        for chunks in (1, 2, 7, 8, 9, 15, 16, 17, 63, 64, 100):
-            n = lib.items(blocks, chunks)
-            assert n < (chunks + 8) * blocks
-            seen, xcd = set(), {}
-            for i in range(n):
-                lib.item(i, blocks, chunks, C.byref(b), C.byref(c))
-                assert 0 <= b.value < blocks and c.value >= 0
-                if c.value >= chunks:
-                    continue
-                assert (b.value, c.value) not in seen
-                seen.add((b.value, c.value))
-                if chunks >= 8:
-                    assert xcd.setdefault(c.value, i % 8) == i % 8
-            assert len(seen) == blocks * chunks
+    """Also: what an XCD has is at most an eighth more than its share, one workgroup a CU where a share is that; groups of a chunk stay on one XCD."""
+    for rows, spans, heads, d_latent, n_cu, room in random_calls(300, 3):
+        p = split(lib, rows, spans, min(heads, 128), d_latent, n_cu, room)
+        if p["items"] > 30000:
+            continue
+        work = workgroups(lib, p)
+        real = [w for w in work if w is not None]
+        assert len(set(real)) == len(real) == sum(chunks * blocks for _, chunks, _, blocks, _ in p["segs"])
+        share = -(-len(real) // 8)
+        longest = -(-len(work) // 8)
+        assert longest <= share + max(1, share // 8)
+        assert longest <= n_cu // 8 or share > n_cu // 8
+        where = {}
+        for i, w in enumerate(work):
+            if w is not None:
+                seg, block, chunk = w
+                where.setdefault((seg, chunk, block % placed(lib, p["segs"][seg][0])[1]), set()).add(i % 8)
+        assert all(len(v) == 1 for v in where.values())
+
+
+def test_blocks_of_a_chunk_go_together_where_there_is_enough_else(lib):
+    """32 requests with two blocks each in five chunks: every chunk's blocks on one XCD.  Ranges that stay in L2: one by one."""
+    p = split(lib, [8] * 32, [2600] * 32, 16)
+    assert all(placed(lib, v)[0] == blocks for v, _, _, blocks, _ in p["segs"])
+    for rows, spans, heads in (([128], [4224], 64), ([2] * 8, [900] * 8, 128)):
+        p = split(lib, rows, spans, heads)
+        assert all(placed(lib, v)[0] == 1 for v, *_ in p["segs"])
+        assert p["items"] == sum(chunks * blocks for _, chunks, _, blocks, _ in p["segs"])
 
 
 def test_one_row_of_a_short_range_is_not_split(lib):
