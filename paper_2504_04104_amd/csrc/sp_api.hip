@@ -56,8 +56,7 @@ struct Workspace {
 
 inline int elt_bytes(int dtype) { return dtype == SP_BF16 ? 2 : 4; }
 
-// Partial rows that the latent attention's cuts may take (sp_latent_plan.h): of every request's query rows as many as blocks cut into chunks
-// for all CUs hold.
+// Partial rows that the latent attention's cuts may take (sp_latent_plan.h): two and a half times those of 256 workgroups of 64 rows.
 constexpr size_t LATENT_UNITS = 40960;
 
 // The workspace of a latent stage: the output head's and the attention's.
