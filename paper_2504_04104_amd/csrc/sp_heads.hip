@@ -133,13 +133,12 @@ __global__ void __launch_bounds__(256) k_head_append(AppendArgs a, FwdBatch b) {
     const int depth = a.tables[req].depth[node];
     slot = sp_phys_slot(a.g, req, m.base, m.P + node);
     // The angle in double precision, whole turns taken off there: positions of tens of thousands keep full float accuracy.
-    if ((int)threadIdx.x < half) {
+    if ((int)threadIdx.x < pairs) {
       const double pos = (double)(m.P + depth);
       const double turns = pos * (a.rope.on ? a.rope.freq[threadIdx.x] : exp2(-(2.0 * (double)threadIdx.x / (double)a.d_head) * a.log2_theta)) * 0.15915494309189535;
       const float ang = (float)((turns - rint(turns)) * 6.283185307179586);
-      const bool turns_at_all = (int)threadIdx.x < pairs;
-      s_cs[threadIdx.x] = turns_at_all ? cosf(ang) * a.rope.gain : 1.f;
-      s_cs[half + threadIdx.x] = turns_at_all ? sinf(ang) * a.rope.gain : 0.f;
+      s_cs[threadIdx.x] = cosf(ang) * a.rope.gain;
+      s_cs[half + threadIdx.x] = sinf(ang) * a.rope.gain;
     }
     __syncthreads();
     cs = s_cs;
@@ -165,14 +164,21 @@ __global__ void __launch_bounds__(256) k_head_append(AppendArgs a, FwdBatch b) {
       v[i] = y * co[i] + x * si[i];
     }
   } else if (rotated && !halves) {
+    // (dims is a multiple of 8: four columns turn or pass together.  By a cosine of 1 and a sine of 0 what is not finite would reach
+    // the column beside it)
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const float ua = u[2 * i], ub = u[2 * i + 1], va = v[2 * i], vb = v[2 * i + 1];
-      const float uc = cs[ca / 2 + i], us = cs[half + ca / 2 + i], vc = cs[cb / 2 + i], vs = cs[half + cb / 2 + i];
-      u[2 * i] = ua * uc - ub * us;
-      u[2 * i + 1] = ub * uc + ua * us;
-      v[2 * i] = va * vc - vb * vs;
-      v[2 * i + 1] = vb * vc + va * vs;
+      if (ca < a.rope.dims) {
+        const float co = cs[ca / 2 + i], si = cs[half + ca / 2 + i];
+        u[2 * i] = ua * co - ub * si;
+        u[2 * i + 1] = ub * co + ua * si;
+      }
+      if (cb < a.rope.dims) {
+        const float co = cs[cb / 2 + i], si = cs[half + cb / 2 + i];
+        v[2 * i] = va * co - vb * si;
+        v[2 * i + 1] = vb * co + va * si;
+      }
     }
   }
   if (!on) return;
