@@ -367,7 +367,9 @@ int sp_latent_append(sp_stage* stage, int32_t layer, int32_t n_req, const int32_
 /* Tree attention of one layer in the latent space, the same rows, order and errors as sp_stage_attention: q [sum n_nodes][n_q_heads][d_latent +
  * d_rope], out [sum n_nodes][n_q_heads][d_latent] = softmax(scale * q . row) over the rows of the committed context, the node itself and
  * its ancestors, times those rows' latents.  Sums and softmax statistics are float32; the softmax's weights are rounded to bf16 before
- * they meet the latents, and divided by the sum of the rounded ones.  q and out are 16-byte aligned device memory and may not overlap.
+ * they meet the latents, and divided by the sum of the rounded ones.  A score of minus infinity is a weight of zero, and its slot counts
+ * as nothing, whatever it holds; one of plus infinity or NaN, or no other score than minus infinity, makes the row's result NaN.  q and out
+ * are 16-byte aligned device memory and may not overlap.
  * Uses the stage's workspace.  A call that the caller captures keeps the trees' sizes and prefix lengths of then. */
 int sp_latent_attention(sp_stage* stage, int32_t layer, int32_t n_req, const int32_t* req_ids /*host*/,
                         const int32_t* first_node /*host*/, const int32_t* n_nodes /*host*/, const void* q, void* out, sp_stream stream);

@@ -178,7 +178,8 @@ __global__ void __launch_bounds__(256) k_latent_attn_simple(LatentAttnArgs a, At
     if ((threadIdx.x & 63) == 0) s_red[wave] = m;
     __syncthreads();
     const float mn = fmaxf(fmaxf(fmaxf(s_red[0], s_red[1]), fmaxf(s_red[2], s_red[3])), mx);
-    const float corr = mx == -INFINITY ? 0.f : __expf(mx - mn), p = seen ? __expf(sc - mn) : 0.f;
+    // (minus infinity is a weight of zero also where there is nothing else yet, whose largest score it then is)
+    const float corr = mx == -INFINITY ? 0.f : __expf(mx - mn), p = sc == -INFINITY ? 0.f : __expf(sc - mn);
     mx = mn;
     s_p[threadIdx.x] = p;
     l = l * corr + p;
@@ -188,7 +189,7 @@ __global__ void __launch_bounds__(256) k_latent_attn_simple(LatentAttnArgs a, At
       const int col = k * 256 + threadIdx.x;
       if (col >= C) continue;
       float acc = o[k] * corr;
-      // (a slot that nobody sees may hold anything)
+      // (a slot that nobody sees, or whose score is minus infinity, may hold anything)
       for (int i = 0; i < n; ++i)
         if (s_p[i] != 0.f) acc += s_p[i] * bf16_to_f32(reinterpret_cast<const bf16_t*>(plane + s_at[i])[col]);
       o[k] = acc;

@@ -195,7 +195,7 @@ __global__ void __launch_bounds__(64 * LW, 2) k_latent_attn(LatentAttnArgs a, At
     const int pp = row * 64 + ((kb * 2 + (kg >> 1)) ^ swap64(row)) * 16 + (kg & 1) * 8;      // (row + 16: 1024 behind)
     float shift[TQ], sum[TQ], add[TQ];
     f32x4_t sa[TQ], sb[TQ];                        // scores of even and odd tiles
-    bool bad_a = false, bad_b = false;
+    bool bad_a = false, bad_b = false;             // the lane's slots of the tile may hold what is not finite
 #pragma unroll
     for (int t = 0; t < TQ; ++t) { shift[t] = NONE; sum[t] = add[t] = 0.f; }
     auto weights = [&](const f32x4_t (&sv)[TQ], int i) {         // of tile i; returns the largest exponent
@@ -252,8 +252,9 @@ __global__ void __launch_bounds__(64 * LW, 2) k_latent_attn(LatentAttnArgs a, At
           shift[t] = now;
         }
         weights(before, i - 1);
-        if (bad_before) {
-          // values that are not finite count as nothing for those who do not see them (those who do have scores that are none)
+        if (__builtin_amdgcn_ballot_w64(bad_before)) {
+          // Values that are not finite count as nothing: for those who do not see them, and where the score is minus infinity.  Those who see
+          // them have no other score but that, plus infinity or NaN, of which the last two make the weight NaN, and with it the row.
           for (int u = lane; u < SUB * 256; u += 64) {
             u32x4_t* p = reinterpret_cast<u32x4_t*>(prev + (u >> 8) * SUB_B + kb * 4096) + (u & 255);
             u32x4_t v = *p;
@@ -272,7 +273,6 @@ __global__ void __launch_bounds__(64 * LW, 2) k_latent_attn(LatentAttnArgs a, At
       for (int t = 0; t < TQ; ++t) sum[t] += add[t];
       if (i >= tiles) return;
       const int k0 = c0 + i * LK + kb * 16;
-      bad = false;
       if (k0 + 16 > P || k0 + 16 > c1) {
         // (what is not finite in a row of the cache shows in all of its scores)
         float odd = 0.f;
@@ -280,7 +280,7 @@ __global__ void __launch_bounds__(64 * LW, 2) k_latent_attn(LatentAttnArgs a, At
         for (int t = 0; t < TQ; ++t)
 #pragma unroll
           for (int j = 0; j < 4; ++j) odd += sv[t][j] * 0.f;
-        bad = __builtin_amdgcn_ballot_w64(odd != odd) != 0;
+        bad = odd != odd;
         const int n0 = k0 - P;
 #pragma unroll
         for (int t = 0; t < TQ; ++t) {
@@ -293,10 +293,16 @@ __global__ void __launch_bounds__(64 * LW, 2) k_latent_attn(LatentAttnArgs a, At
 #pragma unroll
           for (int j = 0; j < 4; ++j) sv[t][j] = (seen >> j) & 1u ? sv[t][j] : -INFINITY;
         }
+      } else {
+        // (everyone sees the sixteen slots: only a score of minus infinity leaves a row of results that another's value could spoil)
+        float low = INFINITY;
+#pragma unroll
+        for (int t = 0; t < TQ; ++t) low = fminf(fminf(fminf(low, sv[t][0]), fminf(sv[t][1], sv[t][2])), sv[t][3]);
+        bad = low == -INFINITY;
       }
       if (i > 0) {                                 // (the first tile is taken again anyway)
         const float top = weights(sv, i);
-        if ((bad || __builtin_amdgcn_ballot_w64(top > FAR)) && lane == 0) s_redo = i;
+        if (__builtin_amdgcn_ballot_w64(bad || top > FAR) && lane == 0) s_redo = i;
       }
       lds_done();
       bare_barrier();                              // the tile's weights are there, the next tile is, nobody reads the one before
