@@ -333,11 +333,13 @@ int sp_stage_set_rope(sp_stage* stage, const sp_rope* rope /*host, nullable*/);
  *
  * A latent stage is a stage with such a cache, for models whose other parts the caller computes.  In its sp_config: dtype SP_BF16,
  * n_kv_heads 1, d_head = d_latent + d_rope, rope_theta and rms_eps as ever, d_ff not looked at, flags SP_FLAG_PAGED_KV and
- * SP_FLAG_SIMPLE_KERNELS; d_model is that of hidden rows (sp_kv_compact, verification).  Matrix-core kernels cover d_latent 256 and 512 with
+ * SP_FLAG_SIMPLE_KERNELS, kv_slots up to SP_LATENT_MAX_SLOTS (else SP_E_UNSUPPORTED: slots are counted in 32 bits, a tile past the last
+ * one included); d_model is that of hidden rows (sp_kv_compact, verification).  Matrix-core kernels cover d_latent 256 and 512 with
  * d_rope 32 and 64, plain ones every multiple of 8 up to 1024 and 128.  The slab is [layer][slot][d_latent + d_rope].
  * Requests, trees, pruning, compaction, pages and verification (the output head; vocabulary matrix row-major) are those of every stage;
  * sp_stage_forward, sp_stage_append, sp_stage_attention, sp_kv_store, sp_kv_load and sp_stage_set_head_norms return SP_E_UNSUPPORTED,
  * as the sp_latent_ calls do on other stages. */
+#define SP_LATENT_MAX_SLOTS (1 << 30)
 typedef struct sp_latent {
   int32_t d_latent;
   int32_t d_rope;

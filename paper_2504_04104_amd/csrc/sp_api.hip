@@ -129,7 +129,7 @@ int check_latent(const sp_config* c, const sp_latent* l) {
   if (!(c->rms_eps > 0.f) || !(c->rope_theta > 1.f) || !(l->scale > 0.f) || !std::isfinite(l->scale)) return SP_E_INVALID;
   if (c->flags & ~(SP_FLAG_PAGED_KV | SP_FLAG_SIMPLE_KERNELS | SP_FLAG_NO_GRAPHS)) return SP_E_UNSUPPORTED;
   if (c->dtype != SP_BF16 || c->d_model % 8 || c->n_q_heads > 1024) return SP_E_UNSUPPORTED;
-  if (l->d_latent % 8 || l->d_latent > 1024 || l->d_rope % 8 || l->d_rope > 2 * SP_ROPE_PAIRS || c->kv_slots > 0x7fffffff) return SP_E_UNSUPPORTED;
+  if (l->d_latent % 8 || l->d_latent > 1024 || l->d_rope % 8 || l->d_rope > 2 * SP_ROPE_PAIRS || c->kv_slots > SP_LATENT_MAX_SLOTS) return SP_E_UNSUPPORTED;
   if (l->norms)
     for (int i = 0; i < c->n_layers; ++i)
       if (!l->norms[i] || ((uintptr_t)l->norms[i] & 15)) return SP_E_INVALID;
