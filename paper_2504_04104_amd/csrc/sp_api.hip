@@ -59,8 +59,11 @@ inline int elt_bytes(int dtype) { return dtype == SP_BF16 ? 2 : 4; }
 // Partial rows that the latent attention's cuts may take (sp_latent_plan.h): two and a half times those of 256 workgroups of 64 rows.
 constexpr size_t LATENT_UNITS = 40960;
 
-// The workspace of a latent stage: the output head's and the attention's.
-Workspace carve_latent(const sp_config& c, int d_latent, char* base) {
+// Whether a latent stage's attention runs on the matrix cores.
+inline bool latent_on_mfma(const sp_config& c, const LatentDims& d) { return !(c.flags & SP_FLAG_SIMPLE_KERNELS) && sp_latent_attn_covers(d); }
+
+// The workspace of a latent stage: the output head's, and where the attention may cut its ranges, that one's.
+Workspace carve_latent(const sp_config& c, const LatentDims& d, char* base) {
   Workspace w;
   const size_t MB = align_up((size_t)c.max_batch_nodes, 16);
   size_t off = 0;
@@ -71,8 +74,8 @@ Workspace carve_latent(const sp_config& c, int d_latent, char* base) {
   w.xn = take(MB * c.d_model * 2);
   w.part_floats = (MB > 1024 ? MB : 1024) * (size_t)c.d_model;
   w.part = (float*)take(w.part_floats * sizeof(float));
-  w.attn_units = LATENT_UNITS;
-  w.attn_part = (float*)take(w.attn_units * (size_t)(d_latent + 2) * sizeof(float));
+  w.attn_units = latent_on_mfma(c, d) ? LATENT_UNITS : 0;
+  w.attn_part = (float*)take(w.attn_units * (size_t)(d.d_latent + 2) * sizeof(float));
   w.total = off;
   return w;
 }
@@ -413,7 +416,7 @@ int sp_latent_query_sizes(const sp_config* cfg, const sp_latent* latent, sp_size
   out->kv_plane_bytes = (size_t)cfg->kv_slots * out->kv_row_bytes;
   out->kv_bytes = (size_t)cfg->n_layers * out->kv_plane_bytes;
   out->tables_bytes = tables_meta_bytes(*cfg) + align_up((size_t)cfg->max_requests * sizeof(ReqTables)) + page_table_bytes(*cfg);
-  out->workspace_bytes = carve_latent(*cfg, latent->d_latent, nullptr).total;
+  out->workspace_bytes = carve_latent(*cfg, {cfg->n_q_heads, latent->d_latent, latent->d_rope}, nullptr).total;
   return SP_OK;
 }
 
@@ -520,7 +523,7 @@ int sp_latent_stage_create(const sp_config* cfg, const sp_latent* latent, const 
   s->lat = {cfg->n_q_heads, latent->d_latent, latent->d_rope};
   s->lat_scale = latent->scale;
   if (latent->norms) s->lat_norms.assign(latent->norms, latent->norms + cfg->n_layers);
-  s->ws = carve_latent(*cfg, latent->d_latent, (char*)buffers->workspace);
+  s->ws = carve_latent(*cfg, s->lat, (char*)buffers->workspace);
   s->geom.planes = cfg->n_layers;
   s->rope = plain_rope(latent->d_rope);
   s->fast = !(cfg->flags & SP_FLAG_SIMPLE_KERNELS) && cfg->d_model % 256 == 0;       // (the output head's kernels)
@@ -1356,7 +1359,7 @@ int sp_latent_attention(sp_stage* s, int32_t layer, int32_t n_req, const int32_t
   AttnPlan plan;
   plan_segments(s, b, nullptr, plan);
   const LatentAttnArgs a = {(const bf16_t*)q, (bf16_t*)out, s->d_tables, s->geom, layer, d, s->lat_scale, s->ws.attn_part};
-  const bool fast = !(s->cfg.flags & SP_FLAG_SIMPLE_KERNELS) && sp_latent_attn_covers(d);
+  const bool fast = latent_on_mfma(s->cfg, d);
   if (fast && !latent_split(plan, d.n_heads, d.d_latent, s->n_cu, s->ws.attn_units)) return SP_E_CAPACITY;
   ProfScope p(s, SP_K_ATTENTION, (hipStream_t)stream);
   const hipError_t e = fast ? sp_launch_latent_attn(a, plan, b.n_rows, (hipStream_t)stream) : sp_launch_latent_attn_simple(a, plan, b.n_rows, (hipStream_t)stream);

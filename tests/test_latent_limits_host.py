@@ -15,3 +15,18 @@ def test_slots_that_32_bits_count_with_a_tile_to_spare(c, r):
         page = dict(flags=sp.SP_FLAG_PAGED_KV, page=32, slots=slots // 32 * 32)
         if page["slots"] > 1 << 30:
             assert sizes(c=c, r=r, **page)[0] == UNSUPPORTED, slots
+
+
+def test_partial_rows_only_where_ranges_are_cut():
+    """Matrix-core kernels: room for 40960 partial rows of d_latent + 2 floats.  Plain kernels cut nothing: room for the output head
+    alone, which a latent's size does not change."""
+    def workspace(**kw):
+        rc, sz = sizes(**kw)
+        assert rc == OK
+        return sz.workspace_bytes
+    head = workspace(c=8, r=8)
+    for c, r in ((512, 64), (512, 32), (256, 64), (256, 32)):
+        assert workspace(c=c, r=r) == head + 40960 * (c + 2) * 4
+        assert workspace(c=c, r=r, flags=sp.SP_FLAG_SIMPLE_KERNELS) == head
+    for c, r in ((1024, 128), (512, 128), (136, 64), (1024, 8)):
+        assert workspace(c=c, r=r) == workspace(c=c, r=r, flags=sp.SP_FLAG_SIMPLE_KERNELS) == head
