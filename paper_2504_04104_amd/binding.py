@@ -262,6 +262,14 @@ class Rope:
             args = (args + (1.0, 1.0, 1.0))[:4]
         _check(load_library().sp_rope_frequencies(dims, theta, kind, *args, self.c.freq), "sp_rope_frequencies")
 
+    # (a copy's address is its own)
+    def __getstate__(self):
+        return bytes(self.c)
+
+    def __setstate__(self, state):
+        self.c = sp_rope.from_buffer_copy(state)
+        self.at = C.addressof(self.c)
+
     @property
     def freq(self) -> List[float]:
         return self.c.freq[:self.c.dims // 2]
