@@ -1117,6 +1117,16 @@ int sp_stage_forward(sp_stage* s, int32_t n_req, const int32_t* req_ids, const i
 }
 
 // ---- a layer's attention piece by piece ---------------------------------------------------------
+// Waits for the stage's device, which need not be the caller's current one.
+static hipError_t wait_for_device(const sp_stage* s) {
+  int dev = s->device;
+  hipError_t e = hipGetDevice(&dev);
+  if (e == hipSuccess && dev != s->device) e = hipSetDevice(s->device);
+  if (e == hipSuccess) e = hipDeviceSynchronize();
+  if (dev != s->device) (void)hipSetDevice(dev);
+  return e;
+}
+
 int sp_stage_set_head_norms(sp_stage* s, const sp_head_norms* layers) {
   if (!s) return SP_E_INVALID;
   if (s->latent) return SP_E_UNSUPPORTED;
@@ -1127,7 +1137,7 @@ int sp_stage_set_head_norms(sp_stage* s, const sp_head_norms* layers) {
     }
   // calls and replays that are still to run read the gains of before; what was captured does not know the new ones
   if (!s->graphs.empty() || !s->norms.empty()) {
-    const hipError_t e = hipDeviceSynchronize();
+    const hipError_t e = wait_for_device(s);
     if (e != hipSuccess) return hip_fail(s, e);
   }
   if (layers) s->norms.assign(layers, layers + s->cfg.n_layers);
@@ -1284,7 +1294,7 @@ int sp_stage_set_rope(sp_stage* s, const sp_rope* rope) {
   }
   // what was captured may launch other kernels than calls from now on
   if (!s->graphs.empty()) {
-    const hipError_t e = hipDeviceSynchronize();
+    const hipError_t e = wait_for_device(s);
     if (e != hipSuccess) return hip_fail(s, e);
   }
   s->rope = next;
