@@ -11,7 +11,7 @@
 // row, or columns that pass.  Sums over
 // the head and maxima over the eight lanes of a 4-bit group stay in the wave; nothing goes through LDS but the angles' sines.
 // Everything is float32 until the one rounding to the storage type.  Bound by the launch and a chain of lookups (request,
-// its prefix, the node's depth, its page) for a tree level: one row 3.6 us, 64 rows 4.2; 640 rows, 16 MB, 6.8.
+// its prefix, the node's depth, its page) for a tree level: one row 3.3 us, 64 rows 4.0; 640 rows, 16 MB, 6.6.
 #include "sp_launch.h"
 #include "sp_fp4.h"
 
@@ -70,21 +70,28 @@ struct AppendArgs {
   void* q;                  // [rows][n_q * d_head]
   KvGeom g;
   int layer, n_q, n_kv, d_head;
-  StageRope rope;           // (PART: its layout and dims, the angles are in cs)
 };
+// A rotation of the stage's own (SET; PART: its layout and dims, the angles are in cs), or none beside the config's.
+struct NoRope {};
+template <bool SET> struct RopeArg { typedef NoRope type; };
+template <> struct RopeArg<true> { typedef StageRope type; };
 
-// grid: (rows, ceil(heads / (256 / (d_head / 8)))).  T: storage of the rows, and of the cache unless FP4.
-template <typename T, bool FP4, bool PART>
-__global__ void __launch_bounds__(256) k_head_append(AppendArgs a, FwdBatch b) {
+// grid: (rows, ceil(heads / (256 / (d_head / 8)))).  T: storage of the rows, and of the cache unless FP4.  The rotation that a stage
+// is created with has kernels of its own: in one with the others, which look up layout, columns and frequencies, one row takes 4.1 us in place
+// of 3.3, 64 rows 4.6 and 4.0, 640 rows 7.0 and 6.6.
+template <typename T, bool FP4, bool PART, bool SET>
+__global__ void __launch_bounds__(256) k_head_append(AppendArgs a, FwdBatch b, typename RopeArg<SET>::type rope) {
   __shared__ float s_cs[128];
   const int half = a.d_head >> 1, tph = half >> 2, row = blockIdx.x;
   const int head = blockIdx.y * (256 / tph) + threadIdx.x / tph;
   const int t = (threadIdx.x % tph) * 4;
   // The lane's columns: in halves four pairs of the rotated columns, or, behind their lanes, columns that pass; interleaved two
   // pairs and two pairs.
-  const int pairs = a.rope.dims >> 1;
-  const bool halves = a.rope.layout == 0, passes = halves && t >= pairs;
-  const int ca = passes ? a.rope.dims + t - pairs : t, cb = !halves ? half + t : passes ? a.rope.dims + half - pairs + t - pairs : pairs + t;
+  int pairs = half, dims = a.d_head;
+  bool halves = true;
+  if constexpr (SET) { dims = rope.dims; pairs = dims >> 1; halves = rope.layout == 0; }
+  const bool passes = SET && halves && t >= pairs;
+  const int ca = passes ? dims + t - pairs : t, cb = !halves ? half + t : passes ? dims + half - pairs + t - pairs : pairs + t;
   const int heads = a.n_q + 2 * a.n_kv;
   const bool on = head < heads, rotated = head < a.n_q + a.n_kv;
 
@@ -135,10 +142,14 @@ __global__ void __launch_bounds__(256) k_head_append(AppendArgs a, FwdBatch b) {
     // The angle in double precision, whole turns taken off there: positions of tens of thousands keep full float accuracy.
     if ((int)threadIdx.x < pairs) {
       const double pos = (double)(m.P + depth);
-      const double turns = pos * (a.rope.on ? a.rope.freq[threadIdx.x] : exp2(-(2.0 * (double)threadIdx.x / (double)a.d_head) * a.log2_theta)) * 0.15915494309189535;
+      double freq;
+      float gain = 1.f;
+      if constexpr (SET) { freq = rope.freq[threadIdx.x]; gain = rope.gain; }
+      else freq = exp2(-(2.0 * (double)threadIdx.x / (double)a.d_head) * a.log2_theta);
+      const double turns = pos * freq * 0.15915494309189535;
       const float ang = (float)((turns - rint(turns)) * 6.283185307179586);
-      s_cs[threadIdx.x] = cosf(ang) * a.rope.gain;
-      s_cs[half + threadIdx.x] = sinf(ang) * a.rope.gain;
+      s_cs[threadIdx.x] = cosf(ang) * gain;
+      s_cs[half + threadIdx.x] = sinf(ang) * gain;
     }
     __syncthreads();
     cs = s_cs;
@@ -169,12 +180,12 @@ __global__ void __launch_bounds__(256) k_head_append(AppendArgs a, FwdBatch b) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const float ua = u[2 * i], ub = u[2 * i + 1], va = v[2 * i], vb = v[2 * i + 1];
-      if (ca < a.rope.dims) {
+      if (ca < dims) {
         const float co = cs[ca / 2 + i], si = cs[half + ca / 2 + i];
         u[2 * i] = ua * co - ub * si;
         u[2 * i + 1] = ub * co + ua * si;
       }
-      if (cb < a.rope.dims) {
+      if (cb < dims) {
         const float co = cs[cb / 2 + i], si = cs[half + cb / 2 + i];
         v[2 * i] = va * co - vb * si;
         v[2 * i + 1] = vb * co + va * si;
@@ -228,30 +239,34 @@ __global__ void __launch_bounds__(256) k_head_rows(KvGeom g, int req, long long 
 }
 
 // ---- launchers -------------------------------------------------------------------
-template <bool PART>
-static hipError_t go_append(int dtype, const AppendArgs& a, const FwdBatch& b, int M, hipStream_t st) {
+template <bool PART, bool SET>
+static hipError_t go_append(int dtype, const AppendArgs& a, const FwdBatch& b, const typename RopeArg<SET>::type& rope, int M, hipStream_t st) {
   const int per = 256 / (a.d_head / 8);
   const dim3 grid(M, (a.n_q + 2 * a.n_kv + per - 1) / per), block(256);
-  if (dtype == 0) hipLaunchKernelGGL((k_head_append<float, false, PART>), grid, block, 0, st, a, b);
-  else if (a.g.scales) hipLaunchKernelGGL((k_head_append<bf16_t, true, PART>), grid, block, 0, st, a, b);
-  else hipLaunchKernelGGL((k_head_append<bf16_t, false, PART>), grid, block, 0, st, a, b);
+  if (dtype == 0) hipLaunchKernelGGL((k_head_append<float, false, PART, SET>), grid, block, 0, st, a, b, rope);
+  else if (a.g.scales) hipLaunchKernelGGL((k_head_append<bf16_t, true, PART, SET>), grid, block, 0, st, a, b, rope);
+  else hipLaunchKernelGGL((k_head_append<bf16_t, false, PART, SET>), grid, block, 0, st, a, b, rope);
   return hipGetLastError();
 }
+template <bool PART>
+static hipError_t go_append(int dtype, const AppendArgs& a, const FwdBatch& b, const StageRope& rope, int M, hipStream_t st) {
+  return rope.on ? go_append<PART, true>(dtype, a, b, rope, M, st) : go_append<PART, false>(dtype, a, b, NoRope(), M, st);
+}
 
-static_assert(sizeof(AppendArgs) + sizeof(FwdBatch) <= 4096, "kernel arguments");
+static_assert(sizeof(AppendArgs) + sizeof(FwdBatch) + sizeof(StageRope) <= 4096, "kernel arguments");
 hipError_t sp_launch_append_parts(int dtype, const float* part, int S, size_t part_stride, const RowInfo* rows, const float* cs,
                                   const StageRope& rope, const void* gain_q, const void* gain_k, float eps, void* qbuf, KvGeom g,
                                   int layer, int M, int n_q, int n_kv, int d_head, hipStream_t st) {
-  AppendArgs a{part, S, part_stride, rows, cs, nullptr, nullptr, 0., gain_q, gain_k, eps, qbuf, g, layer, n_q, n_kv, d_head, rope};
+  AppendArgs a{part, S, part_stride, rows, cs, nullptr, nullptr, 0., gain_q, gain_k, eps, qbuf, g, layer, n_q, n_kv, d_head};
   FwdBatch none;
   none.n_req = 0; none.n_rows = 0;
-  return go_append<true>(dtype, a, none, M, st);
+  return go_append<true>(dtype, a, none, rope, M, st);
 }
 hipError_t sp_launch_append_rows(int dtype, const void* x, const FwdBatch& b, const ReqMeta* meta, const ReqTables* tables,
                                  double log2_theta, const StageRope& rope, const void* gain_q, const void* gain_k, float eps, void* q,
                                  KvGeom g, int layer, int n_q, int n_kv, int d_head, hipStream_t st) {
-  AppendArgs a{x, 1, 0, nullptr, nullptr, meta, tables, log2_theta, gain_q, gain_k, eps, q, g, layer, n_q, n_kv, d_head, rope};
-  return go_append<false>(dtype, a, b, b.n_rows, st);
+  AppendArgs a{x, 1, 0, nullptr, nullptr, meta, tables, log2_theta, gain_q, gain_k, eps, q, g, layer, n_q, n_kv, d_head};
+  return go_append<false>(dtype, a, b, rope, b.n_rows, st);
 }
 
 template <bool STORE>
