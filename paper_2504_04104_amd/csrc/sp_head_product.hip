@@ -1,8 +1,10 @@
 // Products head by head: out[m][h] = x[m][h] W[h]^T, bf16 with float32 sums.
 //
 // Every weight is used m times and every value of x n times: up to some hundred rows the call is bound by the weights' and results' way
-// through memory, and by its launch.  One row x 16 heads, 128 -> 512: 2.6 us; 64 rows x 64 heads, 512 -> 128: 5.8 (14 MB); 637 x 64, 128 ->
-// 512: 14.5 (60 MB, 4.2 TB/s, two thirds of it results); 2048 x 64 31 (176 MB, 5.7 TB/s).
+// through memory, and by its launch.  One row x 16 heads, 128 -> 512: 3.1 us; 64 rows x 64 heads, 512 -> 128: 7.6 (14 MB; half of the CUs have a
+// workgroup, whose four steps wait for their loads one after the other); 637 x 64, 128 -> 512: 14.6 (61 MB, 4.2 TB/s, two thirds of it results);
+// 2048 x 64 37 (176 MB, 4.7 TB/s).  These are kernels alone over three sets of inputs in turn; pairs below are of one set over and over, which
+// is faster where the caches have it.
 #include "sp_launch.h"
 
 typedef __attribute__((ext_vector_type(16))) float f32x16_t;

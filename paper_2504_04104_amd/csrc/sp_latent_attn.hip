@@ -18,8 +18,8 @@
 // Bound by LDS and the clock under full load (1.75 to 1.83 of 2.4 GHz): a tile of 64 rows takes 1736 cycles where its reads (scores 576 and 160,
 // results 256) and the rows coming in (288) need 1280 at 128 bytes a clock and its products 1088.  A workgroup has 4.5 us beside its
 // tiles (first rows, query rows, results out).  512 + 64 columns: 128 nodes x 64 heads behind 4096 slots 71 to 76 us, 1.05 PFLOP/s (a large
-// library product 1.41), and 8.7 of merge; 64 x 32 behind 2048 21.6 and 5.2; 16 rows behind 512
-// 8.7 and 3.5.
+// library product 1.41), and 8.8 of merge; 64 x 32 behind 2048 22 and 5.2; 16 rows behind 512
+// 9.3 and 3.9; 256 x 128 behind 4096, one chunk, 262 to 272, 1.16 PFLOP/s.  256 + 32: 51 and 6.1, 15.7 and 4.1, 7.0 and 3.3.
 #include "sp_latent_plan.h"
 #include "sp_launch.h"
 

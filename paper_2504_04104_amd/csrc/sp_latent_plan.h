@@ -2,7 +2,7 @@
 #pragma once
 #include "sp_plan.h"
 
-#define LATENT_TILE 64             // slots that a workgroup takes at a time
+#define LATENT_TILE 64             // slots that ranges are cut at multiples of: two of the tiles that a workgroup takes at a time
 #define LATENT_FAR (16 << 20)      // bytes of latents that a call reads from where they do not stay in L2
 
 // Workgroups of a call.  Consecutive ones go round over the eight XCDs: workgroup i is number i / 8 of those of XCD i % 8.  A request's work is
@@ -42,9 +42,11 @@ inline int latent_place(AttnPlan& plan, int most) {
   return longest;
 }
 // Groups of up to four blocks where the rows that the call reads are too many for the L2s, 4 MB each, to have a chunk when it is asked for
-// again, and the XCDs stay nearly level (32 requests of 1 to 8 nodes x 16 heads, 75 MB: 33.2 us, 36.6 one by one; 80 query rows behind 32749 slots
-// 26.5 and 29.9); else one by one (64 nodes x 32 heads behind 2048, 2 MB: 28.1, in groups of 32 30.0; 8 requests of 1 to 2 nodes x 128 heads, 6 MB:
-// 22.5 in blocks of 64, in groups 24.2).
+// again, and the XCDs stay nearly level (us a call on one set of rows over and over: 32 requests of 1 to 8 nodes x 16 heads, 75 MB, 33.2, one
+// by one 36.6; 80 query rows behind 32749 slots 26.5 and 29.9); else one by one (64 nodes x 32 heads behind 2048, 2 MB: 28.1, in groups of 32
+// 30.0; 8 requests of 1 to 2 nodes x 128 heads, 6 MB: in blocks of 64 22.5, in groups 24.2, in the blocks of 32 that the rule below
+// takes 21.2 and 22.3, where an order that asks for no XCD took 19.8: the one case measured that this placement costs).  Pairs are of one
+// run; between runs and cards a call moves by up to a tenth.
 inline void latent_place(AttnPlan& plan, long long items, int n_cu, long long bytes) {
   int most = 1;
   if (bytes > LATENT_FAR)
@@ -79,12 +81,16 @@ inline size_t latent_cut(AttnPlan& plan, int H, int d_latent, int rows, int len,
   return units;
 }
 
-// Blocks of 32 or 64 query rows and chunks of the ranges, by the time that they would take: a tile of 64 slots is 1.3 us of a workgroup of
-// 32 rows and 1.75 of one of 64 (d_latent 512; what LDS gives a clock bounds both), a workgroup has 4.5 us beside its tiles, a CU
-// room for one; chunks cost the merge, a launch and the partial rows on their way out and back.  Both sides, us a call, best cut of each:
+// Blocks of 32 or 64 query rows and chunks of the ranges, by the time that they would take: 64 slots are 1.3 us of a workgroup of 32 rows
+// and 1.75 of one of 64 (d_latent 512; what LDS gives a clock bounds blocks of 64, and not those of 32: half of their scores' LDS reads left
+// out, for timing, took 5 % off), a workgroup has 4.5 us beside its tiles, a CU room for one; chunks cost the merge, a launch and the
+// partial rows on their way out and back.  Both sides, us a call, best cut of each:
 // 16 rows behind 512 slots 12.7 in blocks of 32 and 13.3 of 64; 80 behind 32749 24.8 and 25.9; 2048 behind 2048 29.5 and 28.1; 32
 // requests' 16 to 128 behind 512 to 4096 42.5 and 35.9; 8192 behind 4096 90.4 (a chunk) and 79.1 (two).  What is picked is within 8 % of the
-// best of all cuts there.  False: the partial rows do not fit.
+// best of all cuts there.  At d_latent 256 a tile is taken for 0.575 of 512's, which was not fitted by itself: what is picked is within 7 %
+// of the best cut (16 rows behind 512 10.8 in blocks of 32 and 11.1 of 64; 80 behind 32749 18.6 and 20.3; 2048 behind 2048 18.4 and 18.6;
+// 1280 each of 4 requests behind 2000 to 4000 38.8 and 34.4; 8192 behind 4096 58.0 and 50.4).  Rounds are not counted whole: a call of
+// little more than one, or whose partial rows would not fit, is cut less than would be best.  False: the partial rows do not fit.
 inline bool latent_split(AttnPlan& plan, int H, int d_latent, int n_cu, size_t room) {
   int tiles[SP_BATCH], longest = 1;
   for (int i = 0; i < plan.n_seg; ++i) {

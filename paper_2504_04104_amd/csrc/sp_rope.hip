@@ -34,7 +34,8 @@ template <> struct Vec<bf16_t, 8> {
 
 // A workgroup takes a.rows_per rows: the cosines and sines of all their pairs first (the angle in double precision, whole turns
 // taken off there), then V columns a thread at a time together with V that they are paired with, or with V others that pass.  A stream in
-// and out: 32749 rows of 8 heads of 128, bf16, 134 MB, 21.6 us, 6.2 TB/s (a large copy 5.1); one row 2.9.
+// and out: 32749 rows of 8 heads of 128, bf16, 134 MB, 22.7 us, 5.9 TB/s (a large copy 5.1), float32, 16384 rows, 21.8; one row 2.5 and 2.7
+// (kernels alone, three sets of inputs in turn; pairs below of one set over and over).
 // As many rows as have a piece for every thread: 64 heads 1 row at a time 64 rows 4.0 us, 8192 41.0, 8 at a time 14.8 and 45.8; 8 heads 4 at a
 // time 64 rows 3.2, 8192 7.2, 32749 21.6, 1 at a time 3.1, 9.7 and 28.4.
 #define ROTATE_ROWS 8                              // at most
